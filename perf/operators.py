@@ -102,9 +102,10 @@ def draw(rng):
         M = max(1, min(M, MOST_VALUES[op] // (K + N), int(MOST_FLOPS[op] / (2.0 * K * N))))
         return _case(op, M, G=G, K=K, N=N, dtype=dtype, pad=pad, act=rng.choice(["none", "silu"]),
                      train=rng.random() < 0.6, untyped=rng.choice([0.0, 0.0, 0.03]))
+    # 8-bit operands, results in bfloat16
     K, N, G = width(64, 2048), width(64, 2048), between(1, 64)
     M = max(1, min(between(1, 262144), MOST_VALUES[op] // (K + N), int(MOST_FLOPS[op] / (2.0 * K * N))))
-    return _case(op, M, G=G, K=K, N=N, dtype=dtype, pad=16 if pad == 8 else pad, untyped=rng.choice([0.0, 0.0, 0.03]))
+    return _case(op, M, G=G, K=K, N=N, dtype="bfloat16", pad=16 if pad == 8 else pad, untyped=rng.choice([0.0, 0.0, 0.03]))
 
 
 # ------------------------------------------------------------------ inputs
