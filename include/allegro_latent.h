@@ -1,0 +1,150 @@
+/*
+ * allegro_latent.h -- C ABI of the operators of the scalar (latent) track (gfx950).
+ *
+ * An Allegro layer updates scalar features by an MLP with a residual
+ * (allegro_layer.h, step 6; arxiv 2504.16068, Table I and Appendix
+ * "Mixed-Precision Architecture").  The operators here serve models whose
+ * update depends on the type of the edge or atom and whose latents are wide or
+ * deep: rows are grouped by type, multiplied by the weights of their type,
+ * normalised with the residual's addition, and in inference multiplied in 8
+ * bits.  They need no plan and live in liballegro_latent.so.
+ *
+ * Notation
+ *   M rows (edges or atoms), G types; K and N columns
+ *   r      a row; type(r) its type; rows without a type (any value outside
+ *          0 .. G-1, such as padding) belong to no group
+ *   rows   int32 [M]: the rows in order of (type, r), those without a type last
+ *   offsets int64 [G+1]: group g is rows[offsets[g]] .. rows[offsets[g+1] - 1];
+ *          offsets[0] = 0, and offsets[G] rows have a type
+ *   act    the identity, or SiLU(a) = a / (1 + exp(-a))
+ *
+ * Operations (exact definitions; values are reached up to rounding)
+ *   product           Y[r] = act(X[r]) W[type(r)],  Y[r] = 0 without a type
+ *   its gradients     dX[r] = act'(X[r]) * (dY[r] W[type(r)]^T)  (0 without a type)
+ *                     dW[g] = sum over r of type g of act(X[r])^T dY[r]
+ *   norm              s = x + residual,  rstd = 1 / sqrt(mean(s^2) + eps),
+ *                     y = s * rstd * w
+ *   its gradients     t = dy * w,  u = s * rstd,
+ *                     dx = rstd (t - u mean(t u)) + ds
+ *                     dw = sum over rows of dy * u
+ *                     (dx is the gradient of x and of the residual alike)
+ *   norm in 8 bits    for each row and block b of 128 columns (the last may be
+ *                     shorter) scale = max(max |y| / 448, 2^-126) and
+ *                     q = y / scale rounded to nearest, ties to even
+ *   8-bit product     Y[r][n] = sum over blocks b of xs[r][b] ws[g][n / 128][b]
+ *                               sum over k in b of X[r][k] W[g][n][k]
+ *
+ * Types
+ *   dtype ALLEGRO_F32 or ALLEGRO_BF16 is that of every tensor of rows and of W
+ *   and dW of the products; w, rstd, dw of the norm and all scales are fp32;
+ *   8-bit values have 4 exponent and 3 mantissa bits, no infinities and largest
+ *   value 448 ("e4m3fn").  Sums, norms and statistics are held in fp32 and
+ *   rounded to dtype once, when an output is written; with ALLEGRO_BF16 the
+ *   products round act(X) to bf16 as their operand when act is SiLU.  fp32
+ *   products keep fp32 accuracy, 8-bit ones that of their bf16 output.  Infinities and NaN propagate as in the
+ *   formulas.
+ *
+ * Memory and ownership
+ *   Tensors are caller-owned device memory.  A tensor of rows has unit column
+ *   stride and the row stride given with it, in elements and at least its
+ *   width; W, dW, w, dw, rstd, scales, offsets and rows are contiguous.
+ *   Pointers are aligned to their element; 16-byte aligned rows (pointer, row
+ *   stride and width) take the fast paths.  Outputs are overwritten and alias
+ *   nothing.  Workspaces are 16-byte aligned and hold nothing between calls;
+ *   calls that share one must not overlap.  Nothing is allocated per call.
+ *
+ *   offsets and rows are read on the device: offsets out of order or range and
+ *   rows outside 0 .. M-1 cause no access out of bounds, but the outputs of the
+ *   rows concerned are then unspecified.  Each row must be listed once.
+ *
+ * Execution and errors follow allegro_tp.h: calls are asynchronous on `stream`
+ * (a hipStream_t; NULL = the default stream), do not synchronise, may be
+ * captured into graphs, and return ALLEGRO_OK or a negative code with
+ * allegro_latent_last_error().  Host checks: null or misaligned pointers,
+ * negative sizes, row strides below the width, M >= 2^31, widths outside
+ * 1 .. 65536, G outside 1 .. 1024, unknown dtype or act, workspaces that are too
+ * small.  M == 0 succeeds: weight gradients and offsets are zero, nothing else
+ * is written.  Every sum has a fixed order: results are bit-identical run to run
+ * on one kind of device.
+ */
+#ifndef ALLEGRO_LATENT_H
+#define ALLEGRO_LATENT_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "allegro_tp.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum { ALLEGRO_F32 = 0, ALLEGRO_BF16 = 1 };        /* dtype */
+enum { ALLEGRO_ACT_NONE = 0, ALLEGRO_ACT_SILU = 1 }; /* act */
+
+/* Thread-local message of the last failed call of this header's functions. */
+const char *allegro_latent_last_error(void);
+
+/* Device bytes of the workspace of allegro_group_rows (host arithmetic). */
+int allegro_group_rows_workspace(int64_t M, int G, size_t *bytes);
+
+/* offsets [G+1] and rows [M] from type int32 [M]: a stable counting sort. */
+int allegro_group_rows(int64_t M, int G, const int32_t *type, int64_t *offsets, int32_t *rows,
+                       void *workspace, size_t workspace_bytes, void *stream);
+
+/* Y [M][N] from X [M][K] and W [G][K][N].  rows may be NULL: group g is then
+ * rows offsets[g] .. offsets[g+1] - 1 of X and Y themselves. */
+int allegro_grouped_matmul(int dtype, int act, int64_t M, int K, int N, int G,
+                           const int64_t *offsets, const int32_t *rows, const void *X, int64_t ldx,
+                           const void *W, void *Y, int64_t ldy, void *stream);
+
+/* Device bytes of the workspace of allegro_grouped_matmul_backward (host
+ * arithmetic; needed for dW only). */
+int allegro_grouped_matmul_workspace(int64_t M, int K, int N, int G, size_t *bytes);
+
+/* dX [M][K] and dW [G][K][N] from dY [M][N].  Either may be NULL and is then
+ * not computed; without dW the workspace may be NULL. */
+int allegro_grouped_matmul_backward(int dtype, int act, int64_t M, int K, int N, int G,
+                                    const int64_t *offsets, const int32_t *rows, const void *X,
+                                    int64_t ldx, const void *W, const void *dY, int64_t lddy,
+                                    void *dX, int64_t lddx, void *dW, void *workspace,
+                                    size_t workspace_bytes, void *stream);
+
+/* y [M][C], total [M][C] (= x + residual) and rstd [M] from x [M][C], residual
+ * [M][C] and w [C].  residual, total and rstd may be NULL (without a residual
+ * the total is x).  y is the norm of the unrounded sum. */
+int allegro_rms_norm_forward(int dtype, int64_t M, int C, float eps, const void *x, int64_t ldx,
+                             const void *residual, int64_t ldr, const float *w, void *total,
+                             int64_t ldt, void *y, int64_t ldy, float *rstd, void *stream);
+
+/* The same norm with its output in 8 bits: q [M][C] and scale [M][(C+127)/128]. */
+int allegro_rms_norm_fp8(int dtype, int64_t M, int C, float eps, const void *x, int64_t ldx,
+                         const void *residual, int64_t ldr, const float *w, void *total,
+                         int64_t ldt, void *q, int64_t ldq, float *scale, void *stream);
+
+/* Device bytes of the workspace of allegro_rms_norm_backward (host arithmetic). */
+int allegro_rms_norm_workspace(int64_t M, int C, size_t *bytes);
+
+/* dx [M][C] and dw [C] from the forward's total (s) and rstd, dy [M][C] and the
+ * gradient dtotal [M][C] that reaches s along the residual (NULL: none). */
+int allegro_rms_norm_backward(int dtype, int64_t M, int C, const void *total, int64_t ldt,
+                              const float *w, const float *rstd, const void *dy, int64_t lddy,
+                              const void *dtotal, int64_t lddt, void *dx, int64_t lddx, float *dw,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* Y [M][N] in bf16 from 8-bit X [M][K] with scales xs [M][(K+127)/128] and
+ * 8-bit W [G][N][K] with scales ws [G][(N+127)/128][(K+127)/128].  offsets may
+ * be NULL with G == 1: every row is then in the one group (rows is ignored).
+ * The 8-bit matrix instructions add each 8 products in units of 2^-13 of the
+ * largest (typically 2e-6 of a sum's terms, at most 7 2^-13 of them), the rest is
+ * in fp32: hence no fp32 output. */
+int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G,
+                               const int64_t *offsets, const int32_t *rows, const void *X,
+                               int64_t ldx, const float *xs, const void *W, const float *ws,
+                               void *Y, int64_t ldy, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* ALLEGRO_LATENT_H */

@@ -1,9 +1,11 @@
 """MI355X-native Allegro channel-wise tensor product (arxiv 2504.16068, §II.D).
 
 The compute lives in liballegro_tp.so (hand-written HIP for gfx950 behind the
-C ABI of include/allegro_tp.h and include/allegro_layer.h); this package is its
-build script and a thin ctypes binding with the same entry-point names.  Importing the binding raises
-if the library has not been built: there is no CPU fallback.
+C ABI of include/allegro_tp.h and include/allegro_layer.h) and in
+liballegro_latent.so (the operators of the latent track,
+include/allegro_latent.h); this package is their build scripts and a thin ctypes
+binding with the same entry-point names.  Importing the binding raises
+if a library has not been built: there is no CPU fallback.
 """
 
 from .binding import (  # noqa: F401
@@ -33,4 +35,21 @@ from .binding import (  # noqa: F401
     allegro_tp_plan_create,
     allegro_tp_plan_destroy,
     layer_weight_shapes,
+)
+from .latent import (  # noqa: F401
+    ALLEGRO_ACT_NONE,
+    ALLEGRO_ACT_SILU,
+    ALLEGRO_BF16,
+    ALLEGRO_F32,
+    allegro_group_rows,
+    allegro_group_rows_workspace,
+    allegro_grouped_matmul,
+    allegro_grouped_matmul_backward,
+    allegro_grouped_matmul_fp8,
+    allegro_grouped_matmul_workspace,
+    allegro_latent_last_error,
+    allegro_rms_norm_backward,
+    allegro_rms_norm_forward,
+    allegro_rms_norm_fp8,
+    allegro_rms_norm_workspace,
 )
