@@ -151,38 +151,58 @@ __device__ __forceinline__ void put8(u32x4 *lds, int r, int c, const float (&v)[
 }
 
 // A thread's share of the rows of a tile whose contraction runs along memory:
-// 16-byte pieces tid % 8 of rows tid / 8 + 32 i.
-template <class T, int ROWS, bool VEC>
+// 16-byte pieces tid % 8 of rows tid / 8 + 32 i.  Every load is issued, without a
+// condition: a piece that crosses the end of its row (n elements) is loaded from
+// n - PE on and shifted down in put(), in the last step alone.
+template <class T, int ROWS>
 struct Along {
-  static constexpr int NP = ROWS / 32, PE = Kind<T>::PE;
+  static constexpr int NP = ROWS / 32, PE = Kind<T>::PE, KS = Kind<T>::KS;
   u32x4 v[NP];
-  // row(i): pointer to the row's first element (or null); n: elements of a row
+  // row(i): pointer to the first element of row tid / 8 + 32 i
   template <class Row>
   __device__ __forceinline__ void load(Row row, int k0, int n, int tid) {
     const int k = k0 + PE * (tid % 8);
+    if (n >= PE) {
+      const unsigned at = unsigned(k < n - PE ? k : n - PE);
+#pragma unroll
+      for (int i = 0; i < NP; ++i) v[i] = *reinterpret_cast<const u32x4_any *>(row(i) + at);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NP; ++i) {
+        v[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int e = 0; e < PE - 1; ++e)
+          if (k == 0 && e < n) {
+            if constexpr (sizeof(T) == 4)
+              v[i][e] = __builtin_bit_cast(uint32_t, row(i)[e]);
+            else
+              v[i][e / 2] |= uint32_t(row(i)[e]) << (16 * (e % 2));
+          }
+      }
+    }
+  }
+  // the elements from n on become zero
+  __device__ __forceinline__ void cut(int k0, int n, int tid) {
+    const int k = k0 + PE * (tid % 8), by = k < n - PE ? 0 : k - (n - PE);
+    if (n < PE) return;
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      const T *p = row(i);
-      v[i] = u32x4{0, 0, 0, 0};
-      if constexpr (VEC) {
-        if (p && k < n) v[i] = *reinterpret_cast<const u32x4 *>(p + k);
-      } else if (p) {
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (k + e < n) v[i][e] = __builtin_bit_cast(uint32_t, p[k + e]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (k + e < n) v[i][e / 2] |= uint32_t(p[k + e]) << (16 * (e % 2));
-        }
+      u32x4 a = v[i];
+      if constexpr (sizeof(T) == 2) {
+        if (by & 1) a = u32x4{a[0] >> 16 | a[1] << 16, a[1] >> 16 | a[2] << 16, a[2] >> 16 | a[3] << 16, a[3] >> 16};
       }
+      constexpr int E = 4 / int(sizeof(T));
+      if (by & E) a = u32x4{a[1], a[2], a[3], 0};
+      if (by & (2 * E)) a = u32x4{a[2], a[3], 0, 0};
+      if (by >= PE) a = u32x4{0, 0, 0, 0};
+      v[i] = a;
     }
   }
   // into LDS rows base + slot(tid / 8 + 32 i)
   template <int R, bool WIDE>
-  __device__ __forceinline__ void put(u32x4 *lds, int base, bool act, float scale, int tid) const {
-    constexpr int C = Kind<T>::KS / 8;
+  __device__ __forceinline__ void put(u32x4 *lds, int base, bool act, float scale, int k0, int n, int tid) {
+    constexpr int C = KS / 8;
+    if (k0 + KS > n) cut(k0, n, tid);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       const int r = base + slot_of<WIDE>(tid / 8 + 32 * i);
@@ -192,12 +212,14 @@ struct Along {
         for (int e = 0; e < 4; ++e) {
           const uint32_t bits = v[i][e];  // a bit cast of the vector's element itself gives element 0
           x[e] = __builtin_bit_cast(float, bits);
-          if (act) x[e] = silu(x[e]);
-          x[e] *= scale;
+        }
+        if (act) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = silu(x[e]);
         }
         uint32_t h[2], m[2], l[2];
-        split2(x[0], x[1], h[0], m[0], l[0]);
-        split2(x[2], x[3], h[1], m[1], l[1]);
+        split2(scale * x[0], scale * x[1], h[0], m[0], l[0]);
+        split2(scale * x[2], scale * x[3], h[1], m[1], l[1]);
         u32x2 *d = reinterpret_cast<u32x2 *>(lds) + tid % 2;
         d[2 * chunk_at<C, R>(0, r, tid % 8 / 2)] = u32x2{h[0], h[1]};
         d[2 * chunk_at<C, R>(1, r, tid % 8 / 2)] = u32x2{m[0], m[1]};
@@ -217,33 +239,46 @@ struct Along {
 };
 
 // A thread's share of a tile whose contraction runs across memory rows: EPT
-// consecutive steps of one column, or with PAIR of two neighbouring 16-bit ones.
-template <class T, int COLS, bool PAIR>
+// consecutive steps of one column, or of 16-bit tiles 128 wide of two neighbouring
+// ones.  The memory rows are the same for a whole wave, so their addresses are
+// scalar.  Columns past the last one read the last: they reach no output.
+template <class T, int COLS>
 struct Across {
+  static constexpr bool PAIR = sizeof(T) == 2 && COLS == 128;
   static constexpr int LANES = PAIR ? COLS / 2 : COLS, EPT = Kind<T>::KS * LANES / kThreads;
-  static_assert(EPT % 8 == 0, "whole chunks");
-  static __device__ __forceinline__ int part(int tid) { return tid / LANES; }
+  static_assert(EPT % 8 == 0 && LANES % kWave == 0, "whole chunks, one part to a wave");
+  static __device__ __forceinline__ int part(int tid) { return __builtin_amdgcn_readfirstlane(tid / LANES); }
   static __device__ __forceinline__ int col(int tid) { return tid % LANES * (PAIR ? 2 : 1); }
   uint32_t v[EPT];
-  // row(i): pointer to element 0 of step part * EPT + i (or null); c: the column, below n
+  // row(i): pointer to element 0 of step part * EPT + i, the same for all lanes; c: the column, n of them
   template <class Row>
   __device__ __forceinline__ void load(Row row, int c, int n) {
+    if (PAIR && n > 1) {
+      const unsigned at = unsigned(c < n - 2 ? c : n - 2);
 #pragma unroll
-    for (int i = 0; i < EPT; ++i) {
-      const T *p = row(i);
-      v[i] = 0;
-      if (p && c < n) {
-        if constexpr (PAIR)
-          v[i] = *reinterpret_cast<const uint32_t *>(p + c);
-        else if constexpr (sizeof(T) == 4)
-          v[i] = __builtin_bit_cast(uint32_t, p[c]);
+      for (int i = 0; i < EPT; ++i) v[i] = *reinterpret_cast<const u32_any *>(row(i) + at);
+      if (n & 1) {  // the last column's pair holds it in its upper half
+#pragma unroll
+        for (int i = 0; i < EPT; ++i) v[i] = c == n - 1 ? v[i] >> 16 : v[i];
+      }
+    } else {
+      const unsigned at = unsigned(c < n ? c : n - 1);
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) {
+        if constexpr (sizeof(T) == 4)
+          v[i] = __builtin_bit_cast(uint32_t, row(i)[at]);
         else
-          v[i] = p[c];
+          v[i] = row(i)[at];
       }
     }
   }
+  // valid: bit i is set if step part * EPT + i exists; the others become zero
   template <int R, bool WIDE>
-  __device__ __forceinline__ void put(u32x4 *lds, int base, bool act, float scale, int tid) const {
+  __device__ __forceinline__ void put(u32x4 *lds, int base, bool act, float scale, uint32_t valid, int tid) {
+    if (valid != (EPT == 32 ? ~0u : (1u << EPT) - 1)) {
+#pragma unroll
+      for (int i = 0; i < EPT; ++i) v[i] = valid >> i & 1 ? v[i] : 0u;
+    }
     const int c0 = part(tid) * (EPT / 8);
 #pragma unroll
     for (int q = 0; q < EPT / 8; ++q) {
@@ -257,7 +292,10 @@ struct Across {
           for (int e = 0; e < 4; ++e) {
             const uint32_t a = v[8 * q + 2 * e], b = v[8 * q + 2 * e + 1];
             o[e] = s ? __builtin_amdgcn_perm(b, a, 0x07060302) : __builtin_amdgcn_perm(b, a, 0x05040100);
-            if (act)
+          }
+          if (act) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
               o[e] = bf16_pair(silu(__builtin_bit_cast(float, o[e] << 16)),
                                silu(__builtin_bit_cast(float, o[e] & 0xffff0000u)));
           }
@@ -265,9 +303,10 @@ struct Across {
         } else {
           float x[8];
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] = __builtin_bit_cast(float, v[8 * q + e]);
-            if (act) x[e] = silu(x[e]);
+          for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, v[8 * q + e]);
+          if (act) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = silu(x[e]);
           }
           put8<T, R>(lds, r, c0 + q, x, scale);
         }
@@ -275,6 +314,13 @@ struct Across {
     }
   }
 };
+
+// Bits i < n of the steps first + i that are below end.
+__device__ __forceinline__ uint32_t steps_below(int64_t first, int64_t end, int n) {
+  const int64_t left = end - first;
+  const uint32_t all = n == 32 ? ~0u : (1u << n) - 1;
+  return left >= n ? all : left <= 0 ? 0u : (1u << left) - 1;
+}
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -353,12 +399,12 @@ __device__ __forceinline__ void multiply_again(f32x4 (&acc)[MI][NI], int64_t K, 
   });
 }
 
-// Stores the 4 (or, of two products, 8) consecutive values that a lane holds of
-// a row, columns n .. of N.
+// Loads or stores the 4 (or, of two products, 8) consecutive values that a lane
+// holds of a row; `left` columns exist from the first on.
 template <int W>
-__device__ __forceinline__ void store_row(float *p, const float *v, int left, bool vec) {
-  if (vec && left >= W) {
-    *reinterpret_cast<f32x4 *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+__device__ __forceinline__ void store_row(float *p, const float *v, int left) {
+  if (left >= W) {
+    *reinterpret_cast<u32x4_any *>(p) = __builtin_bit_cast(u32x4, f32x4{v[0], v[1], v[2], v[3]});
   } else {
 #pragma unroll
     for (int i = 0; i < W; ++i)
@@ -366,17 +412,36 @@ __device__ __forceinline__ void store_row(float *p, const float *v, int left, bo
   }
 }
 template <int W>
-__device__ __forceinline__ void store_row(uint16_t *p, const float *v, int left, bool vec) {
-  if (vec && left >= W) {
+__device__ __forceinline__ void store_row(uint16_t *p, const float *v, int left) {
+  if (left >= W) {
     if constexpr (W == 8)
-      *reinterpret_cast<u32x4 *>(p) =
+      *reinterpret_cast<u32x4_any *>(p) =
           u32x4{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
     else
-      *reinterpret_cast<uint2 *>(p) = make_uint2(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]));
+      *reinterpret_cast<u32x2_any *>(p) = u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
   } else {
 #pragma unroll
     for (int i = 0; i < W; ++i)
       if (i < left) p[i] = bf16_bits(v[i]);
+  }
+}
+template <int W, class T>
+__device__ __forceinline__ void load_row(const T *p, float *v, int left) {
+  if (left >= W) {
+    const u32x4 a = *reinterpret_cast<const u32x4_any *>(p);  // 16 bytes in both types
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t bits = a[i];
+      if constexpr (sizeof(T) == 4) {
+        v[i] = __builtin_bit_cast(float, bits);
+      } else {
+        v[2 * i] = __builtin_bit_cast(float, bits << 16);
+        v[2 * i + 1] = __builtin_bit_cast(float, bits & 0xffff0000u);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] = i < left ? to_f32(p[i]) : 0.f;
   }
 }
 
@@ -420,8 +485,8 @@ struct ProductArgs {
   int64_t mt;  // upper bound of the row tiles
 };
 
-template <class T, int TN, bool WT, bool VEC>
-__global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs g) {
+template <class T, int TN, bool WT>
+__global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
   constexpr int P = Kind<T>::P, KS = Kind<T>::KS, R = kTileRows + TN, C = KS / 8;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int MI = 4, NI = TN / 32;
@@ -444,20 +509,27 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs g) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = srow[tid / 8 + 32 * i];
-    xr[i] = r < 0 ? nullptr : x + int64_t(r) * g.ldx;
+    xr[i] = x + (r < 0 ? 0 : int64_t(r) * g.ldx);  // rows past the end are multiplied but not stored
   }
-  constexpr bool PAIR = !F32 && VEC;
-  using WLoad = std::conditional_t<WT, Along<T, TN, VEC>, Across<T, TN, PAIR>>;
-  Along<T, kTileRows, VEC> a;
+  using WLoad = std::conditional_t<WT, Along<T, TN>, Across<T, TN>>;
+  Along<T, kTileRows> a;
   WLoad bw;
+  int wr[TN / 32];  // W transposed: the rows' offsets from column n0's
+  if constexpr (WT) {
+    w += int64_t(n0) * K;
+#pragma unroll
+    for (int i = 0; i < TN / 32; ++i) {
+      const int n = tid / 8 + 32 * i;
+      wr[i] = (n < N - n0 ? n : N - n0 - 1) * K;
+    }
+  }
   auto load = [&](int k0) {
     a.load([&](int i) { return xr[i]; }, k0, K, tid);
     if constexpr (WT) {
-      bw.load([&](int i) { const int n = n0 + tid / 8 + 32 * i; return n < N ? w + int64_t(n) * K : nullptr; }, k0, K,
-              tid);
+      bw.load([&](int i) { return w + wr[i]; }, k0, K, tid);
     } else {
       const int kp = k0 + WLoad::part(tid) * WLoad::EPT;
-      bw.load([&](int i) { return kp + i < K ? w + int64_t(kp + i) * N : nullptr; }, n0 + WLoad::col(tid), N);
+      bw.load([&](int i) { return w + int64_t(kp + i < K ? kp + i : K - 1) * N + n0; }, WLoad::col(tid), N - n0);
     }
   };
   f32x4 acc[MI][NI];
@@ -470,8 +542,12 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs g) {
   load(0);
   for (int k0 = 0; k0 < K; k0 += KS) {
     lds_sync<4>();  // the previous step has been read
-    a.template put<R, false>(lds, 0, g.act, xs, tid);
-    bw.template put<R, !F32>(lds, kTileRows, false, kScale, tid);
+    a.template put<R, false>(lds, 0, g.act, xs, k0, K, tid);
+    if constexpr (WT)
+      bw.template put<R, !F32>(lds, kTileRows, false, kScale, k0, K, tid);
+    else
+      bw.template put<R, !F32>(lds, kTileRows, false, kScale,
+                               steps_below(k0 + WLoad::part(tid) * WLoad::EPT, K, WLoad::EPT), tid);
     lds_sync<4>();
     if (k0 + KS < K) load(k0 + KS);
     multiply<T, R, MI, NI>(lds, wm, kTileRows + wn, 1.f, acc, l);
@@ -487,7 +563,7 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs g) {
           },
           [&](int j, int64_t k) {
             const int n = n0 + wn + 16 * j + l % 16;
-            return n >= N ? 0.f : WT ? w[int64_t(n) * K + k] : w[k * N + n];
+            return n >= N ? 0.f : WT ? w[int64_t(n - n0) * K + k] : w[k * N + n];
           });
     } else {
       const float u = l % 2 ? -kUnscale : kUnscale;
@@ -511,11 +587,12 @@ __global__ __launch_bounds__(kThreads) void product_kernel(ProductArgs g) {
 #pragma unroll
       for (int e = 0; e < W; ++e) v[e] = acc[i][j + e / 4][e % 4];
       if (pre) {
+        float p[W];
+        load_row<W>(pre + int64_t(r) * g.ldp + n, p, N - n);
 #pragma unroll
-        for (int e = 0; e < W; ++e)
-          if (n + e < N) v[e] *= silu_grad(to_f32(pre[int64_t(r) * g.ldp + n + e]));
+        for (int e = 0; e < W; ++e) v[e] *= silu_grad(p[e]);
       }
-      store_row<W>(y + int64_t(r) * g.ldy + n, v, N - n, VEC);
+      store_row<W>(y + int64_t(r) * g.ldy + n, v, N - n);
     }
   }
 }
@@ -539,8 +616,8 @@ struct WeightArgs {
 
 // Range k of a group of several goes to slot 2 (offsets[g] >> shift) + k: such a
 // group has more than 1 << shift rows, so the next one's slots start behind it.
-template <class T, int TK, int TN, bool VEC>
-__global__ __launch_bounds__(kThreads) void weight_kernel(WeightArgs g) {
+template <class T, int TK, int TN>
+__global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
   constexpr int P = Kind<T>::P, KS = Kind<T>::KS, R = TK + TN, C = KS / 8;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int MI = TK / 32, NI = TN / 32;
@@ -556,25 +633,24 @@ __global__ __launch_bounds__(kThreads) void weight_kernel(WeightArgs g) {
   const int64_t end = t.m0 + (int64_t(1) << g.shift) < t.end ? t.m0 + (int64_t(1) << g.shift) : t.end;
   const int k0 = int(b % tiles) / g.nt * TK, n0 = int(b % tiles) % g.nt * TN, K = g.K, N = g.N;
   const T *x = static_cast<const T *>(g.x), *dy = static_cast<const T *>(g.dy);
-  // 16-bit pairs where a wave covers the whole tile's width
-  constexpr bool PX = !F32 && VEC && TK == 128, PY = !F32 && VEC && TN == 128;
-  using XLoad = Across<T, TK, PX>;
-  using YLoad = Across<T, TN, PY>;
+  using XLoad = Across<T, TK>;
+  using YLoad = Across<T, TN>;
   XLoad xa;
   YLoad ya;
-  // the rows of a step are the same for all lanes of a wave: scalar loads of the
-  // list and scalar row addresses
-  auto row_of = [&](int64_t i) -> int64_t {
+  auto row_of = [&](int64_t i) -> int {
     if (i >= end) return -1;
     const int64_t r = g.rows ? int64_t(g.rows[i]) : i;
-    return r < 0 || r >= g.M ? -1 : r;
+    return r < 0 || r >= g.M ? -1 : int(r);
   };
-  const int xpart = __builtin_amdgcn_readfirstlane(XLoad::part(tid)), ypart = __builtin_amdgcn_readfirstlane(YLoad::part(tid));
-  auto load = [&](int64_t m) {
-    xa.load([&](int i) -> const T * { const int64_t r = row_of(m + xpart * XLoad::EPT + i); return r < 0 ? nullptr : x + r * g.ldx; },
-            k0 + XLoad::col(tid), K);
-    ya.load([&](int i) -> const T * { const int64_t r = row_of(m + ypart * YLoad::EPT + i); return r < 0 ? nullptr : dy + r * g.lddy; },
-            n0 + YLoad::col(tid), N);
+  // the rows of a step are the same for all lanes: lane i loads row i of the step
+  // two ahead, the addresses are formed with its value in a scalar register
+  const int xpart = XLoad::part(tid) * XLoad::EPT, ypart = YLoad::part(tid) * YLoad::EPT;
+  auto load = [&](int rows) {
+    const int r = rows < 0 ? 0 : rows;
+    xa.load([&](int i) { return x + int64_t(__builtin_amdgcn_readlane(r, xpart + i)) * g.ldx + k0; }, XLoad::col(tid),
+            K - k0);
+    ya.load([&](int i) { return dy + int64_t(__builtin_amdgcn_readlane(r, ypart + i)) * g.lddy + n0; },
+            YLoad::col(tid), N - n0);
   };
   f32x4 acc[MI][NI];
 #pragma unroll
@@ -583,13 +659,21 @@ __global__ __launch_bounds__(kThreads) void weight_kernel(WeightArgs g) {
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int wk = TK / 2 * (wave % 2), wn = TN / 2 * (wave / 2);
   float sign = 1.f;
-  if (t.m0 < end) load(t.m0);
+  const int lk = l % KS;
+  int rows = row_of(t.m0 + lk);
+  uint64_t valid = __ballot(rows >= 0);
+  if (t.m0 < end) load(rows);
+  rows = row_of(t.m0 + KS + lk);
   for (int64_t m = t.m0; m < end; m += KS) {
     lds_sync<4>();
-    xa.template put<R, false>(lds, 0, g.act, sign * kScale, tid);
-    ya.template put<R, false>(lds, TK, false, kScale, tid);
+    xa.template put<R, false>(lds, 0, g.act, sign * kScale, uint32_t(valid >> xpart) & steps_below(0, KS, XLoad::EPT), tid);
+    ya.template put<R, false>(lds, TK, false, kScale, uint32_t(valid >> ypart) & steps_below(0, KS, YLoad::EPT), tid);
     lds_sync<4>();
-    if (m + KS < end) load(m + KS);
+    valid = __ballot(rows >= 0);
+    if (m + KS < end) {
+      load(rows);
+      rows = row_of(m + 2 * KS + lk);
+    }
     multiply<T, R, MI, NI>(lds, wk, TK + wn, sign, acc, l);
     sign = -sign;
   }
@@ -616,7 +700,6 @@ __global__ __launch_bounds__(kThreads) void weight_kernel(WeightArgs g) {
     }
   }
   const int64_t k_first = (t.m0 - begin) >> g.shift;
-  const bool vec = N % 4 == 0;  // whole groups of four columns, and (checked on the host) an aligned dw
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int k = k0 + wk + 16 * i + l % 16;
@@ -628,9 +711,9 @@ __global__ __launch_bounds__(kThreads) void weight_kernel(WeightArgs g) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = acc[i][j][e];
       if (only)
-        store_row<4>(static_cast<T *>(g.dw) + (int64_t(t.g) * K + k) * N + n, v, N - n, VEC && vec);
+        store_row<4>(static_cast<T *>(g.dw) + (int64_t(t.g) * K + k) * N + n, v, N - n);
       else
-        store_row<4>(g.part + (2 * (begin >> g.shift) + k_first) * g.slot + int64_t(k) * N + n, v, N - n, vec);
+        store_row<4>(g.part + (2 * (begin >> g.shift) + k_first) * g.slot + int64_t(k) * N + n, v, N - n);
     }
   }
 }
@@ -700,7 +783,6 @@ struct ProductF8Args {
   int64_t ldy;
   int nt;
   int64_t mt;
-  bool yvec;  // 16-byte rows of y
 };
 
 // A step is one block of 128 along K: one matrix instruction (16 x 16 x 128) forms
@@ -709,8 +791,8 @@ struct ProductF8Args {
 // below 2^-13 of it (measured; the 16 x 16 x 32 one does the same at half the
 // rate), 2e-6 of the terms' magnitudes for normally distributed operands: far
 // below the bf16 output's 2^-8, and the reason that there is no fp32 output.
-template <int TN, bool VEC>
-__global__ __launch_bounds__(kThreads) void product_f8_kernel(ProductF8Args g) {
+template <int TN>
+__global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g) {
   constexpr int KS = 128, C = KS / 16, R = kTileRows + TN, MI = 4, NI = TN / 32;
   __shared__ u32x4 lds[R * C];
   __shared__ int srow[kTileRows];
@@ -739,22 +821,35 @@ __global__ __launch_bounds__(kThreads) void product_f8_kernel(ProductF8Args g) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int r = srow[tid / 8 + 32 * i];
-    xr[i] = r < 0 ? nullptr : g.x + int64_t(r) * g.ldx;
+    xr[i] = g.x + (r < 0 ? 0 : int64_t(r) * g.ldx);
   }
   int mrow[MI];
 #pragma unroll
   for (int i = 0; i < MI; ++i) mrow[i] = srow[wm + 16 * i + l % 16];
+  // 16 bytes from k on, as Along does: pieces that cross the row's end are loaded
+  // before it and shifted when they are used
+  const int at_last = K - 16;
   auto load16 = [&](const uint8_t *p, int k) {
     u32x4 v = {0, 0, 0, 0};
-    if (!p) return v;
-    if constexpr (VEC) {
-      if (k < K) v = *reinterpret_cast<const u32x4 *>(p + k);
+    if (at_last >= 0) {
+      v = *reinterpret_cast<const u32x4_any8 *>(p + unsigned(k < at_last ? k : at_last));
     } else {
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (k + e < K) v[e / 4] |= uint32_t(p[k + e]) << (8 * (e % 4));
+      for (int e = 0; e < 15; ++e)
+        if (k == 0 && e < K) v[e / 4] |= uint32_t(p[e]) << (8 * (e % 4));
     }
     return v;
+  };
+  auto cut = [&](u32x4 a, int k) {
+    const int by = k < at_last ? 0 : k - at_last, bits = 8 * (by % 4);
+    if (at_last < 0) return a;
+    u32x4 o;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_alignbit(i < 3 ? a[i + 1] : 0u, a[i], bits);
+    if (by & 4) o = u32x4{o[1], o[2], o[3], 0};
+    if (by & 8) o = u32x4{o[2], o[3], 0, 0};
+    if (by >= 16) o = u32x4{0, 0, 0, 0};
+    return o;
   };
   constexpr int NW = TN / 32;
   u32x4 a[4], bw[NW];
@@ -766,11 +861,11 @@ __global__ __launch_bounds__(kThreads) void product_f8_kernel(ProductF8Args g) {
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
       const int n = n0 + tid / 8 + 32 * i;
-      bw[i] = load16(n < N ? w + int64_t(n) * K : nullptr, k);
+      bw[i] = load16(w + int64_t(n < N ? n : N - 1) * K, k);
     }
     sw = ws[k0 / KS];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) sx[i] = mrow[i] < 0 ? 0.f : g.xs[int64_t(mrow[i]) * kb + k0 / KS];
+    for (int i = 0; i < MI; ++i) sx[i] = g.xs[int64_t(mrow[i] < 0 ? 0 : mrow[i]) * kb + k0 / KS];
   };
   f32x4 acc[MI][NI];
 #pragma unroll
@@ -780,6 +875,13 @@ __global__ __launch_bounds__(kThreads) void product_f8_kernel(ProductF8Args g) {
   load(0);
   for (int k0 = 0; k0 < K; k0 += KS) {
     lds_sync<4>();
+    if (k0 + KS > K) {
+      const int k = k0 + 16 * (tid % 8);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = cut(a[i], k);
+#pragma unroll
+      for (int i = 0; i < NW; ++i) bw[i] = cut(bw[i], k);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) lds[chunk_at<C, R>(0, tid / 8 + 32 * i, tid % 8)] = a[i];
 #pragma unroll
@@ -821,26 +923,22 @@ __global__ __launch_bounds__(kThreads) void product_f8_kernel(ProductF8Args g) {
       float v[W];
 #pragma unroll
       for (int e = 0; e < W; ++e) v[e] = acc[i][j + e / 4][e % 4];
-      store_row<W>(y + int64_t(mrow[i]) * g.ldy + n, v, N - n, g.yvec);
+      store_row<W>(y + int64_t(mrow[i]) * g.ldy + n, v, N - n);
     }
   }
 }
 
 // ------------------------------------------------------------- launches
 template <class T, bool WT>
-void launch_product(ProductArgs g, bool vec, hipStream_t s) {
+void launch_product(ProductArgs g, hipStream_t s) {
   const bool narrow = g.N <= 64;
   g.nt = narrow ? 1 : int(cdiv(g.N, 128));
   g.mt = tile_bound(g.M, g.G, kTileShift);
   const dim3 grid(unsigned(g.mt * g.nt)), block(kThreads);
-  if (narrow && vec)
-    hipLaunchKernelGGL((product_kernel<T, 64, WT, true>), grid, block, 0, s, g);
-  else if (narrow)
-    hipLaunchKernelGGL((product_kernel<T, 64, WT, false>), grid, block, 0, s, g);
-  else if (vec)
-    hipLaunchKernelGGL((product_kernel<T, 128, WT, true>), grid, block, 0, s, g);
+  if (narrow)
+    hipLaunchKernelGGL((product_kernel<T, 64, WT>), grid, block, 0, s, g);
   else
-    hipLaunchKernelGGL((product_kernel<T, 128, WT, false>), grid, block, 0, s, g);
+    hipLaunchKernelGGL((product_kernel<T, 128, WT>), grid, block, 0, s, g);
 }
 
 struct WeightShape {
@@ -860,30 +958,22 @@ WeightShape weight_shape(int64_t M, int K, int N) {
   return z;
 }
 
-template <class T, int TK, int TN>
-void launch_weight_tile(const WeightArgs &g, bool vec, hipStream_t s) {
-  const dim3 grid(unsigned(g.ranges * g.kt * g.nt)), block(kThreads);
-  if (vec)
-    hipLaunchKernelGGL((weight_kernel<T, TK, TN, true>), grid, block, 0, s, g);
-  else
-    hipLaunchKernelGGL((weight_kernel<T, TK, TN, false>), grid, block, 0, s, g);
-}
-
 template <class T>
-void launch_weight(WeightArgs g, const WeightShape &z, bool vec, hipStream_t s) {
+void launch_weight(WeightArgs g, const WeightShape &z, hipStream_t s) {
   g.shift = z.shift;
   g.kt = z.kt;
   g.nt = z.nt;
   g.slot = z.slot;
   g.ranges = tile_bound(g.M, g.G, z.shift);
+  const dim3 grid(unsigned(g.ranges * g.kt * g.nt)), block(kThreads);
   if (g.K <= 64 && g.N <= 64)
-    launch_weight_tile<T, 64, 64>(g, vec, s);
+    hipLaunchKernelGGL((weight_kernel<T, 64, 64>), grid, block, 0, s, g);
   else if (g.K <= 64)
-    launch_weight_tile<T, 64, 128>(g, vec, s);
+    hipLaunchKernelGGL((weight_kernel<T, 64, 128>), grid, block, 0, s, g);
   else if (g.N <= 64)
-    launch_weight_tile<T, 128, 64>(g, vec, s);
+    hipLaunchKernelGGL((weight_kernel<T, 128, 64>), grid, block, 0, s, g);
   else
-    launch_weight_tile<T, 128, 128>(g, vec, s);
+    hipLaunchKernelGGL((weight_kernel<T, 128, 128>), grid, block, 0, s, g);
   if (z.slots) {
     const unsigned several = unsigned(std::min<int64_t>(g.G, g.M >> z.shift));
     hipLaunchKernelGGL((weight_sum_kernel<T>), dim3(unsigned(cdiv(int64_t(g.K) * g.N, 256)), several),
@@ -903,11 +993,6 @@ int check_product(int dtype, int act, int64_t M, int K, int N, int G) {
   return ALLEGRO_OK;
 }
 
-// Whether the 16-byte paths hold for a tensor of rows of `width` elements.
-bool whole(const void *p, int64_t ld, int width, int elem) {
-  return width * elem % 16 == 0 && aligned(p, ld * elem, 16);
-}
-
 }  // namespace
 
 extern "C" {
@@ -923,12 +1008,11 @@ int allegro_grouped_matmul(int dtype, int act, int64_t M, int K, int N, int G, c
       (rc = check_rows(X, "X", ldx, K, e)) || (rc = check_ptr(W, "W", e)) || (rc = check_rows(Y, "Y", ldy, N, e)))
     return rc;
   const ProductArgs g{M, K, N, G, offsets, rows, X, ldx, W, Y, ldy, nullptr, 0, act, 0, 0};
-  const bool vec = whole(X, ldx, K, e) && whole(W, N, N, e) && whole(Y, ldy, N, e);
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == ALLEGRO_F32)
-    launch_product<float, false>(g, vec, s);
+    launch_product<float, false>(g, s);
   else
-    launch_product<uint16_t, false>(g, vec, s);
+    launch_product<uint16_t, false>(g, s);
   return after("allegro_grouped_matmul");
 }
 
@@ -974,20 +1058,18 @@ int allegro_grouped_matmul_backward(int dtype, int act, int64_t M, int K, int N,
   if (dX) {
     // the same product with W transposed: the contraction runs along dY's columns
     const ProductArgs g{M, N, K, G, offsets, rows, dY, lddy, W, dX, lddx, act ? X : nullptr, ldx, 0, 0, 0};
-    const bool vec = whole(dY, lddy, N, e) && whole(W, N, N, e) && whole(dX, lddx, K, e);
     if (dtype == ALLEGRO_F32)
-      launch_product<float, true>(g, vec, s);
+      launch_product<float, true>(g, s);
     else
-      launch_product<uint16_t, true>(g, vec, s);
+      launch_product<uint16_t, true>(g, s);
   }
   if (dW) {
     const WeightArgs g{M,  K,    N,  G,    act, 0, offsets, rows, X, ldx, dY, lddy, dW, static_cast<float *>(workspace),
                        0, 0, 0, 0};
-    const bool vec = whole(X, ldx, K, e) && whole(dY, lddy, N, e) && whole(dW, N, N, e);
     if (dtype == ALLEGRO_F32)
-      launch_weight<float>(g, z, vec, s);
+      launch_weight<float>(g, z, s);
     else
-      launch_weight<uint16_t>(g, z, vec, s);
+      launch_weight<uint16_t>(g, z, s);
   }
   return after("allegro_grouped_matmul_backward");
 }
@@ -1010,18 +1092,13 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
                         xs, static_cast<const uint8_t *>(W),
                         ws, static_cast<uint16_t *>(Y),
                         ldy, int(cdiv(N, N <= 64 ? 64 : 128)),
-                        tile_bound(M, G, kTileShift), whole(Y, ldy, N, 2)};
-  const bool vec = whole(X, ldx, K, 1) && whole(W, K, K, 1);
+                        tile_bound(M, G, kTileShift)};
   const dim3 grid(unsigned(g.mt * g.nt)), block(kThreads);
   hipStream_t s = static_cast<hipStream_t>(stream);
-  if (N <= 64 && vec)
-    hipLaunchKernelGGL((product_f8_kernel<64, true>), grid, block, 0, s, g);
-  else if (N <= 64)
-    hipLaunchKernelGGL((product_f8_kernel<64, false>), grid, block, 0, s, g);
-  else if (vec)
-    hipLaunchKernelGGL((product_f8_kernel<128, true>), grid, block, 0, s, g);
+  if (N <= 64)
+    hipLaunchKernelGGL((product_f8_kernel<64>), grid, block, 0, s, g);
   else
-    hipLaunchKernelGGL((product_f8_kernel<128, false>), grid, block, 0, s, g);
+    hipLaunchKernelGGL((product_f8_kernel<128>), grid, block, 0, s, g);
   return after("allegro_grouped_matmul_fp8");
 }
 
