@@ -15,12 +15,13 @@
 // with no sums over groups and no launch before.  Rows without a type are one
 // more group, of zeros.
 //
-// Operand layout.  Tiles lie in LDS as rows of 16-bit (or 8-bit) values along
-// the contraction, 16-byte chunks XOR-swizzled by row so that 8 and 16 lanes on
-// consecutive rows hit distinct banks.  The matrix instructions take W's columns
-// as their rows: lane l then holds 4 consecutive columns of Y's row l % 16 per
-// 16 x 16 product and stores them straight from registers; with 16-bit results
-// two products' columns are interleaved (slot_of) to 8 consecutive ones.
+// Operands.  Every tensor is read 16 bytes at a time along its memory rows.  Where
+// the contraction runs along them (X and, transposed, W) a tile lies in LDS as it
+// is multiplied (Along); where it runs across them (W, and both operands of dW)
+// the transposing LDS loads turn it (Across).  The matrix instructions take the
+// result's columns as their rows: lane l then holds 4 consecutive columns of row
+// l % 16 per 16 x 16 product and stores them straight from registers; with 16-bit
+// results two products' columns are interleaved (column_of) to 8 consecutive ones.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -74,6 +75,21 @@ __device__ __forceinline__ Tile find_tile(const int64_t *__restrict__ offsets, i
   return {g, begin, k < 0 ? end : begin + (k << shift), end};
 }
 
+// The group at `unit` of a line on which group g starts at offsets[g] + cost * g.
+__device__ __forceinline__ Tile find_group(const int64_t *__restrict__ offsets, int G, int64_t M, int64_t unit,
+                                           int64_t cost, int lane) {
+  auto clamped = [&](int i) {
+    const int64_t o = offsets[i];
+    return o < 0 ? int64_t(0) : o > M ? M : o;
+  };
+  int below = 0;
+  for (int i = lane; i <= G; i += kWave) below += clamped(i) + cost * i <= unit;
+  for (int m = kWave / 2; m; m >>= 1) below += __shfl_xor(below, m);
+  const int g = __builtin_amdgcn_readfirstlane(below > 0 ? below - 1 : 0);
+  const int64_t begin = clamped(g), end = g < G ? clamped(g + 1) : M;
+  return {g, begin, begin, end > begin ? end : begin};
+}
+
 __host__ __device__ inline int64_t tile_bound(int64_t M, int G, int shift) { return (M >> shift) + G + 1; }
 
 // Workgroups go round the 8 XCDs: give each XCD consecutive tiles, so that the
@@ -106,18 +122,12 @@ struct Kind<uint16_t> {
   static constexpr int P = 1, KS = 64, PE = 8;
 };
 
-// 16-byte chunk c of row r of plane p of a tile of R rows with C chunks to a row.
-template <int C, int R>
-__device__ __forceinline__ int chunk_at(int p, int r, int c) {
-  const int f = C == 4 ? ((r >> 1) & 3) ^ ((r >> 3) & 1) : (r & 7) ^ ((r >> 3) & 1);
-  return (p * R + r) * C + (c ^ f);
-}
-
-// LDS row of result column n: with 16-bit results, columns 8 q + 4 h + i of 32
-// (i < 4, h < 2) lie at row 16 h + 4 q + i.
+// Result column of row i of the matrix instructions' 16 x 16 product j: with 16-bit
+// results (WIDE) two products share 32 columns so that lane l, which gets rows
+// 4 (l / 16) .. + 3 of each, holds 8 consecutive columns of the two.
 template <bool WIDE>
-__device__ __forceinline__ int slot_of(int n) {
-  return WIDE ? (n & ~31) | ((n >> 2) & 1) << 4 | ((n >> 3) & 3) << 2 | (n & 3) : n;
+__device__ __forceinline__ int column_of(int j, int i) {
+  return WIDE ? 32 * (j / 2) + 8 * (i / 4) + 4 * (j % 2) + i % 4 : 16 * j + i;
 }
 
 __device__ __forceinline__ void split2(float a, float b, uint32_t &h, uint32_t &m, uint32_t &l) {
@@ -127,226 +137,226 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t &h, uint32_t &
   l = bf16_pair(ra - __builtin_bit_cast(float, m << 16), rb - __builtin_bit_cast(float, m & 0xffff0000u));
 }
 
-// Writes 8 consecutive contraction values of LDS row r (chunk c).
-template <class T, int R>
-__device__ __forceinline__ void put8(u32x4 *lds, int r, int c, const float (&v)[8], float scale) {
-  constexpr int C = Kind<T>::KS / 8;
-  if constexpr (sizeof(T) == 4) {
-    u32x4 h, m, l;
+// One 16-byte piece of fp32 values, through SiLU or not, as the three planes' parts.
+__device__ __forceinline__ void split_piece(u32x4 v, bool act, float scale, u32x2 (&o)[3]) {
+  float x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t a, b, d;
-      split2(scale * v[2 * i], scale * v[2 * i + 1], a, b, d);
-      h[i] = a; m[i] = b; l[i] = d;
-    }
-    lds[chunk_at<C, R>(0, r, c)] = h;
-    lds[chunk_at<C, R>(1, r, c)] = m;
-    lds[chunk_at<C, R>(2, r, c)] = l;
-  } else {
-    u32x4 h;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) h[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
-    lds[chunk_at<C, R>(0, r, c)] = h;
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t bits = v[e];  // a bit cast of the vector's element itself gives element 0
+    x[e] = __builtin_bit_cast(float, bits);
   }
+  if (act) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = silu(x[e]);
+  }
+  uint32_t h[2], m[2], l[2];
+  split2(scale * x[0], scale * x[1], h[0], m[0], l[0]);
+  split2(scale * x[2], scale * x[3], h[1], m[1], l[1]);
+  o[0] = u32x2{h[0], h[1]};
+  o[1] = u32x2{m[0], m[1]};
+  o[2] = u32x2{l[0], l[1]};
+}
+__device__ __forceinline__ u32x4 act_piece(u32x4 v, bool act) {  // of bf16 values
+  if (act) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      v[e] = bf16_pair(silu(__builtin_bit_cast(float, v[e] << 16)), silu(__builtin_bit_cast(float, v[e] & 0xffff0000u)));
+  }
+  return v;
 }
 
-// A thread's share of the rows of a tile whose contraction runs along memory:
-// 16-byte pieces tid % 8 of rows tid / 8 + 32 i.  Every load is issued, without a
-// condition: a piece that crosses the end of its row (n elements) is loaded from
-// n - PE on and shifted down in put(), in the last step alone.
-template <class T, int ROWS>
+// Pieces of the elements k .. of rows of n (k below n or not), row(i) pointing to
+// row i's first one.  The loads are issued without a condition: where a piece
+// crosses the row's end the row's last PE elements are loaded, and shifted down
+// by shift_of when they are used.
+template <class T, int NP, class Row>
+__device__ __forceinline__ void load_pieces(u32x4 (&v)[NP], Row row, int k, int n) {
+  constexpr int PE = Kind<T>::PE;
+  if (n >= PE) {
+    const unsigned at = unsigned(k < n - PE ? k : n - PE);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) v[i] = *reinterpret_cast<const u32x4_any *>(row(i) + at);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < NP; ++i) {
+    v[i] = u32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < PE - 1; ++e)
+      if (k == 0 && e < n) {
+        if constexpr (sizeof(T) == 4)
+          v[i][e] = __builtin_bit_cast(uint32_t, row(i)[e]);
+        else
+          v[i][e / 2] |= uint32_t(row(i)[e]) << (16 * (e % 2));
+      }
+  }
+}
+template <class T>
+__device__ __forceinline__ int shift_of(int k, int n) {
+  constexpr int PE = Kind<T>::PE;
+  return n < PE || k < n - PE ? 0 : k - (n - PE);
+}
+// Drops the first `by` elements; zeros follow the last.
+template <class T>
+__device__ __forceinline__ u32x4 shifted(u32x4 a, int by) {
+  if constexpr (sizeof(T) == 2) {
+    if (by & 1) a = u32x4{a[0] >> 16 | a[1] << 16, a[1] >> 16 | a[2] << 16, a[2] >> 16 | a[3] << 16, a[3] >> 16};
+  }
+  constexpr int E = 4 / int(sizeof(T));
+  if (by & E) a = u32x4{a[1], a[2], a[3], 0};
+  if (by & (2 * E)) a = u32x4{a[2], a[3], 0, 0};
+  if (by >= Kind<T>::PE) a = u32x4{0, 0, 0, 0};
+  return a;
+}
+
+// 16-byte chunk c of row r of rows of 4 or 8 chunks (64 or 128 bytes).
+template <int C>
+__device__ __forceinline__ int swizzled(int r, int c) {
+  return r * C + (c ^ (C == 4 ? ((r >> 1) & 3) ^ ((r >> 3) & 1) : (r & 7) ^ ((r >> 3) & 1)));
+}
+
+// A tile of `ROWS` rows (of X, or columns of the result) whose contraction runs
+// along memory.  In LDS: rows of KS 16-bit values, in 16-byte chunks swizzled by
+// row so that 8 and 16 lanes reading one chunk of consecutive rows hit distinct
+// banks.  A thread moves pieces tid % 8 of rows tid / 8 + 32 i.
+template <class T, int ROWS, bool WIDE>
 struct Along {
-  static constexpr int NP = ROWS / 32, PE = Kind<T>::PE, KS = Kind<T>::KS;
+  static constexpr int P = Kind<T>::P, KS = Kind<T>::KS, PE = Kind<T>::PE, NP = ROWS / 32, C = KS / 8;
+  static constexpr int SIZE = P * ROWS * C;  // 16-byte units
   u32x4 v[NP];
-  // row(i): pointer to the first element of row tid / 8 + 32 i
+  // row(i): pointer to the first element of row tid / 8 + 32 i; n elements to a row
   template <class Row>
   __device__ __forceinline__ void load(Row row, int k0, int n, int tid) {
-    const int k = k0 + PE * (tid % 8);
-    if (n >= PE) {
-      const unsigned at = unsigned(k < n - PE ? k : n - PE);
-#pragma unroll
-      for (int i = 0; i < NP; ++i) v[i] = *reinterpret_cast<const u32x4_any *>(row(i) + at);
-    } else {
-#pragma unroll
-      for (int i = 0; i < NP; ++i) {
-        v[i] = u32x4{0, 0, 0, 0};
-#pragma unroll
-        for (int e = 0; e < PE - 1; ++e)
-          if (k == 0 && e < n) {
-            if constexpr (sizeof(T) == 4)
-              v[i][e] = __builtin_bit_cast(uint32_t, row(i)[e]);
-            else
-              v[i][e / 2] |= uint32_t(row(i)[e]) << (16 * (e % 2));
-          }
-      }
-    }
+    load_pieces<T>(v, row, k0 + PE * (tid % 8), n);
   }
-  // the elements from n on become zero
-  __device__ __forceinline__ void cut(int k0, int n, int tid) {
-    const int k = k0 + PE * (tid % 8), by = k < n - PE ? 0 : k - (n - PE);
-    if (n < PE) return;
+  __device__ __forceinline__ void put(u32x4 *lds, bool act, float scale, int k0, int n, int tid) {
+    if (k0 + KS > n) {  // the last step: nothing from n on
+#pragma unroll
+      for (int i = 0; i < NP; ++i) v[i] = shifted<T>(v[i], shift_of<T>(k0 + PE * (tid % 8), n));
+    }
+    // rows 32 apart are swizzled alike
+    const int at = P == 3 ? 2 * swizzled<C>(tid / 8, tid % 8 / 2) + tid % 2 : swizzled<C>(tid / 8, tid % 8);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
-      u32x4 a = v[i];
-      if constexpr (sizeof(T) == 2) {
-        if (by & 1) a = u32x4{a[0] >> 16 | a[1] << 16, a[1] >> 16 | a[2] << 16, a[2] >> 16 | a[3] << 16, a[3] >> 16};
-      }
-      constexpr int E = 4 / int(sizeof(T));
-      if (by & E) a = u32x4{a[1], a[2], a[3], 0};
-      if (by & (2 * E)) a = u32x4{a[2], a[3], 0, 0};
-      if (by >= PE) a = u32x4{0, 0, 0, 0};
-      v[i] = a;
-    }
-  }
-  // into LDS rows base + slot(tid / 8 + 32 i)
-  template <int R, bool WIDE>
-  __device__ __forceinline__ void put(u32x4 *lds, int base, bool act, float scale, int k0, int n, int tid) {
-    constexpr int C = KS / 8;
-    if (k0 + KS > n) cut(k0, n, tid);
+      if constexpr (P == 3) {
+        u32x2 o[3];
+        split_piece(v[i], act, scale, o);
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-      const int r = base + slot_of<WIDE>(tid / 8 + 32 * i);
-      if constexpr (sizeof(T) == 4) {
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t bits = v[i][e];  // a bit cast of the vector's element itself gives element 0
-          x[e] = __builtin_bit_cast(float, bits);
-        }
-        if (act) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) x[e] = silu(x[e]);
-        }
-        uint32_t h[2], m[2], l[2];
-        split2(scale * x[0], scale * x[1], h[0], m[0], l[0]);
-        split2(scale * x[2], scale * x[3], h[1], m[1], l[1]);
-        u32x2 *d = reinterpret_cast<u32x2 *>(lds) + tid % 2;
-        d[2 * chunk_at<C, R>(0, r, tid % 8 / 2)] = u32x2{h[0], h[1]};
-        d[2 * chunk_at<C, R>(1, r, tid % 8 / 2)] = u32x2{m[0], m[1]};
-        d[2 * chunk_at<C, R>(2, r, tid % 8 / 2)] = u32x2{l[0], l[1]};
+        for (int p = 0; p < 3; ++p) reinterpret_cast<u32x2 *>(lds)[at + 2 * C * (p * ROWS + 32 * i)] = o[p];
       } else {
-        u32x4 o = v[i];
-        if (act) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            o[e] = bf16_pair(silu(__builtin_bit_cast(float, o[e] << 16)),
-                             silu(__builtin_bit_cast(float, o[e] & 0xffff0000u)));
-        }
-        lds[chunk_at<C, R>(0, r, tid % 8)] = o;
+        lds[at + C * 32 * i] = act_piece(v[i], act);
       }
     }
   }
+  // Operands of a wave from product j0 on (a whole number of 32 columns if WIDE):
+  // lane l has row l % 16 of product j0 + j and k = 32 kk + 8 (l / 16) ...  The
+  // lane's part of the address is the same for all j up to the product's parity,
+  // and kk flips one of its bits.
+  struct Reader {
+    int base[WIDE ? 2 : 1];
+    __device__ __forceinline__ Reader(int j0, int l) {
+#pragma unroll
+      for (int h = 0; h < (WIDE ? 2 : 1); ++h) base[h] = swizzled<C>(column_of<WIDE>(j0 + h, l % 16), l / 16);
+    }
+    __device__ __forceinline__ bf16x8 get(const u32x4 *lds, int p, int j, int kk) const {
+      const int row = p * ROWS + (WIDE ? 32 * (j / 2) : 16 * j);
+      return __builtin_bit_cast(bf16x8, lds[(base[WIDE ? j % 2 : 0] ^ (4 * kk)) + C * row]);
+    }
+  };
 };
 
-// A thread's share of a tile whose contraction runs across memory rows: EPT
-// consecutive steps of one column, or of 16-bit tiles 128 wide of two neighbouring
-// ones.  The memory rows are the same for a whole wave, so their addresses are
-// scalar.  Columns past the last one read the last: they reach no output.
-template <class T, int COLS>
+// A tile of COLS columns whose contraction runs across memory rows.  In LDS: KS
+// rows of COLS 16-bit values as they come; operands are read with the transposing
+// LDS load, by which 16 lanes turn 4 rows of 16 columns into 4 rows of one column
+// each.  A wave's load touches 4 columns' quads of 16 rows; chunks (and their
+// halves) are swizzled by row so that those 512 bytes lie in all banks twice.
+template <class T, int COLS, bool WIDE>
 struct Across {
-  static constexpr bool PAIR = sizeof(T) == 2 && COLS == 128;
-  static constexpr int LANES = PAIR ? COLS / 2 : COLS, EPT = Kind<T>::KS * LANES / kThreads;
-  static_assert(EPT % 8 == 0 && LANES % kWave == 0, "whole chunks, one part to a wave");
-  static __device__ __forceinline__ int part(int tid) { return __builtin_amdgcn_readfirstlane(tid / LANES); }
-  static __device__ __forceinline__ int col(int tid) { return tid % LANES * (PAIR ? 2 : 1); }
-  uint32_t v[EPT];
-  // row(i): pointer to element 0 of step part * EPT + i, the same for all lanes; c: the column, n of them
+  static constexpr int P = Kind<T>::P, KS = Kind<T>::KS, PE = Kind<T>::PE;
+  static constexpr int PR = COLS / PE, RP = kThreads / PR, NP = KS / RP;  // pieces to a row, rows to a pass
+  static constexpr int SIZE = P * KS * COLS / 8;                          // 16-byte units
+  u32x4 v[NP];
+  static __device__ __forceinline__ int quad_at(int k, int c4) {  // in 8-byte units
+    const int f = COLS == 128 ? (k & 3) << 2 | ((k >> 3) & 1) << 1 : ((k >> 1) & 1) << 2 | ((k >> 3) & 1) << 1;
+    return k * (COLS / 4) + ((((c4 >> 1) ^ f) << 1) | ((c4 & 1) ^ ((k >> 3) & 1)));
+  }
+  static __device__ __forceinline__ int step(int i, int tid) { return tid / PR + i * RP; }
+  static __device__ __forceinline__ int col(int tid) { return tid % PR * PE; }
+  // row(i): pointer to the first of the tile's columns (n of them exist) of step step(i, tid)
   template <class Row>
-  __device__ __forceinline__ void load(Row row, int c, int n) {
-    if (PAIR && n > 1) {
-      const unsigned at = unsigned(c < n - 2 ? c : n - 2);
+  __device__ __forceinline__ void load(Row row, int n, int tid) {
+    load_pieces<T>(v, row, col(tid), n);
+  }
+  // missing: bit i is set if step(i, tid) does not exist and becomes zero
+  __device__ __forceinline__ void put(u32x4 *lds, bool act, float scale, int n, int missing, int tid) {
+    if (n < COLS) {
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) v[i] = *reinterpret_cast<const u32_any *>(row(i) + at);
-      if (n & 1) {  // the last column's pair holds it in its upper half
+      for (int i = 0; i < NP; ++i) v[i] = shifted<T>(v[i], shift_of<T>(col(tid), n));
+    }
+    if (__any(missing)) {
 #pragma unroll
-        for (int i = 0; i < EPT; ++i) v[i] = c == n - 1 ? v[i] >> 16 : v[i];
-      }
-    } else {
-      const unsigned at = unsigned(c < n ? c : n - 1);
+      for (int i = 0; i < NP; ++i) v[i] = missing >> i & 1 ? u32x4{0, 0, 0, 0} : v[i];
+    }
+    // rows of one pass are RP apart: RP = 8 flips the bits of k / 8, 16 and 32 none
+    const int at = quad_at(step(0, tid), tid % PR * (PE / 4));
+    const bool swap = P == 1 && (step(0, tid) >> 3 & 1);  // the halves' order in a 16-byte chunk
 #pragma unroll
-      for (int i = 0; i < EPT; ++i) {
-        if constexpr (sizeof(T) == 4)
-          v[i] = __builtin_bit_cast(uint32_t, row(i)[at]);
-        else
-          v[i] = row(i)[at];
+    for (int i = 0; i < NP; ++i) {
+      const int flip = RP == 8 && i % 2 ? 5 : 0, row = i * RP * (COLS / 4);
+      if constexpr (P == 3) {
+        u32x2 o[3];
+        split_piece(v[i], act, scale, o);
+#pragma unroll
+        for (int p = 0; p < 3; ++p) reinterpret_cast<u32x2 *>(lds)[(at ^ flip) + row + p * KS * (COLS / 4)] = o[p];
+      } else {
+        const u32x4 a = act_piece(v[i], act);
+        lds[(at + row) / 2] = swap ? u32x4{a[2], a[3], a[0], a[1]} : a;
       }
     }
   }
-  // valid: bit i is set if step part * EPT + i exists; the others become zero
-  template <int R, bool WIDE>
-  __device__ __forceinline__ void put(u32x4 *lds, int base, bool act, float scale, uint32_t valid, int tid) {
-    if (valid != (EPT == 32 ? ~0u : (1u << EPT) - 1)) {
-#pragma unroll
-      for (int i = 0; i < EPT; ++i) v[i] = valid >> i & 1 ? v[i] : 0u;
+  // Operands of a wave from product j0 on, as Along::Reader.  Columns 4 j flip bits
+  // of the lane's address; the swizzle repeats every 4 rows of 8 and every 16.
+  struct Reader {
+    int base;
+    __device__ __forceinline__ Reader(int j0, int l) {
+      base = quad_at(8 * (l / 16) + l % 16 / 4, l % 4 * (WIDE ? 2 : 1)) ^ (4 * j0);
     }
-    const int c0 = part(tid) * (EPT / 8);
-#pragma unroll
-    for (int q = 0; q < EPT / 8; ++q) {
-#pragma unroll
-      for (int s = 0; s < (PAIR ? 2 : 1); ++s) {
-        const int r = base + slot_of<WIDE>(col(tid) + s);
-        if constexpr (sizeof(T) == 2) {
-          // 16-bit values are moved as they are, or through SiLU
-          u32x4 o;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const uint32_t a = v[8 * q + 2 * e], b = v[8 * q + 2 * e + 1];
-            o[e] = s ? __builtin_amdgcn_perm(b, a, 0x07060302) : __builtin_amdgcn_perm(b, a, 0x05040100);
-          }
-          if (act) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              o[e] = bf16_pair(silu(__builtin_bit_cast(float, o[e] << 16)),
-                               silu(__builtin_bit_cast(float, o[e] & 0xffff0000u)));
-          }
-          lds[chunk_at<Kind<T>::KS / 8, R>(0, r, c0 + q)] = o;
-        } else {
-          float x[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = __builtin_bit_cast(float, v[8 * q + e]);
-          if (act) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = silu(x[e]);
-          }
-          put8<T, R>(lds, r, c0 + q, x, scale);
-        }
-      }
+    __device__ __forceinline__ bf16x8 get(const u32x4 *lds, int p, int j, int kk) const {
+      typedef short s16x4 __attribute__((ext_vector_type(4)));
+      typedef short s16x8 __attribute__((ext_vector_type(8)));
+      typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+      const u32x2 *q = reinterpret_cast<const u32x2 *>(lds) + (base ^ (WIDE ? 8 * (j / 2) + j % 2 : 4 * j)) +
+                       (p * KS + 32 * kk) * (COLS / 4);
+      const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)q);
+      const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(q + COLS));
+      return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     }
-  }
+  };
 };
-
-// Bits i < n of the steps first + i that are below end.
-__device__ __forceinline__ uint32_t steps_below(int64_t first, int64_t end, int n) {
-  const int64_t left = end - first;
-  const uint32_t all = n == 32 ? ~0u : (1u << n) - 1;
-  return left >= n ? all : left <= 0 ? 0u : (1u << left) - 1;
-}
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
 
-// One contraction step of a wave: MI x NI products of 16 x 16.  The matrix
-// instructions' rows are LDS rows row_n + 16 j + l % 16, their columns LDS rows
-// row_m + 16 i + l % 16.  fp32 sums are added with the factor `sign`.
-template <class T, int R, int MI, int NI>
-__device__ __forceinline__ void multiply(const u32x4 *lds, int row_m, int row_n, float sign, f32x4 (&acc)[MI][NI],
-                                         int l) {
-  constexpr int P = Kind<T>::P, C = Kind<T>::KS / 8;
-  auto frag = [&](int p, int r, int c) { return __builtin_bit_cast(bf16x8, lds[chunk_at<C, R>(p, r, c)]); };
+// One contraction step of a wave: MI x NI products of 16 x 16 of the tiles ML (the
+// instructions' columns) and NL (their rows).  fp32 sums are added with the factor
+// `sign`.
+template <class T, class ML, class NL, int MI, int NI>
+__device__ __forceinline__ void multiply(const u32x4 *m_lds, const u32x4 *n_lds, const typename ML::Reader &m_read,
+                                         const typename NL::Reader &n_read, float sign, f32x4 (&acc)[MI][NI]) {
+  constexpr int P = Kind<T>::P;
 #pragma unroll
-  for (int kk = 0; kk < C / 4; ++kk) {
-    const int c = 4 * kk + l / 16;
+  for (int kk = 0; kk < Kind<T>::KS / 32; ++kk) {
     bf16x8 b[MI][P];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
-      for (int p = 0; p < P; ++p) b[i][p] = frag(p, row_m + 16 * i + l % 16, c);
+      for (int p = 0; p < P; ++p) b[i][p] = m_read.get(m_lds, p, i, kk);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
       bf16x8 a[P];
 #pragma unroll
-      for (int p = 0; p < P; ++p) a[p] = frag(p, row_n + 16 * j + l % 16, c);
+      for (int p = 0; p < P; ++p) a[p] = n_read.get(n_lds, p, j, kk);
       if constexpr (P == 1) {
 #pragma unroll
         for (int i = 0; i < MI; ++i) acc[i][j] = mfma16(a[0], b[i][0], acc[i][j]);
@@ -425,23 +435,28 @@ __device__ __forceinline__ void store_row(uint16_t *p, const float *v, int left)
       if (i < left) p[i] = bf16_bits(v[i]);
   }
 }
-template <int W, class T>
-__device__ __forceinline__ void load_row(const T *p, float *v, int left) {
-  if (left >= W) {
-    const u32x4 a = *reinterpret_cast<const u32x4_any *>(p);  // 16 bytes in both types
+template <int W, class T>  // 16 bytes in both types
+__device__ __forceinline__ u32x4 load_bits(const T *p, int left) {
+  if (left >= W) return *reinterpret_cast<const u32x4_any *>(p);
+  u32x4 v = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t bits = a[i];
-      if constexpr (sizeof(T) == 4) {
-        v[i] = __builtin_bit_cast(float, bits);
-      } else {
-        v[2 * i] = __builtin_bit_cast(float, bits << 16);
-        v[2 * i + 1] = __builtin_bit_cast(float, bits & 0xffff0000u);
-      }
+  for (int i = 0; i < W - 1; ++i)
+    if (i < left) {
+      if constexpr (sizeof(T) == 4)
+        v[i] = __builtin_bit_cast(uint32_t, p[i]);
+      else
+        v[i / 2] |= uint32_t(p[i]) << (16 * (i % 2));
     }
+  return v;
+}
+template <class T>
+__device__ __forceinline__ float value_of(u32x4 v, int e) {
+  if constexpr (sizeof(T) == 4) {
+    const uint32_t bits = v[e];
+    return __builtin_bit_cast(float, bits);
   } else {
-#pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = i < left ? to_f32(p[i]) : 0.f;
+    const uint32_t bits = e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16;
+    return __builtin_bit_cast(float, bits);
   }
 }
 
@@ -478,19 +493,21 @@ struct ProductArgs {
   const void *w;  // [G][K][N], transposed [G][N][K]
   void *y;        // [M][N]
   int64_t ldy;
-  const void *pre;  // y is multiplied with SiLU'(pre), if given ([M][N])
+  const void *pre;  // transposed: y is multiplied with SiLU'(pre), if given ([M][N])
   int64_t ldp;
-  int act;     // SiLU on x
+  int act;     // SiLU on x (not transposed)
   int nt;      // column tiles
   int64_t mt;  // upper bound of the row tiles
 };
 
 template <class T, int TN, bool WT>
 __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
-  constexpr int P = Kind<T>::P, KS = Kind<T>::KS, R = kTileRows + TN, C = KS / 8;
+  constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int MI = 4, NI = TN / 32;
-  __shared__ u32x4 lds[P * R * C];
+  using XTile = Along<T, kTileRows, false>;
+  using WTile = std::conditional_t<WT, Along<T, TN, !F32>, Across<T, TN, !F32>>;
+  __shared__ u32x4 x_lds[XTile::SIZE], w_lds[WTile::SIZE];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
@@ -505,31 +522,31 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
     return;
   }
   const T *x = static_cast<const T *>(g.x), *w = static_cast<const T *>(g.w) + int64_t(t.g) * K * N;
-  const T *xr[4];
+  const T *xr[XTile::NP];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < XTile::NP; ++i) {
     const int r = srow[tid / 8 + 32 * i];
     xr[i] = x + (r < 0 ? 0 : int64_t(r) * g.ldx);  // rows past the end are multiplied but not stored
   }
-  using WLoad = std::conditional_t<WT, Along<T, TN>, Across<T, TN>>;
-  Along<T, kTileRows> a;
-  WLoad bw;
-  int wr[TN / 32];  // W transposed: the rows' offsets from column n0's
-  if constexpr (WT) {
-    w += int64_t(n0) * K;
-#pragma unroll
-    for (int i = 0; i < TN / 32; ++i) {
-      const int n = tid / 8 + 32 * i;
-      wr[i] = (n < N - n0 ? n : N - n0 - 1) * K;
-    }
-  }
+  XTile a;
+  WTile bw;
+  int missing = 0;
   auto load = [&](int k0) {
     a.load([&](int i) { return xr[i]; }, k0, K, tid);
     if constexpr (WT) {
-      bw.load([&](int i) { return w + wr[i]; }, k0, K, tid);
+      bw.load(
+          [&](int i) {
+            const int n = tid / 8 + 32 * i;  // columns past the last read it, and reach no output
+            return w + int64_t(n0) * K + (n < N - n0 ? n : N - n0 - 1) * K;
+          },
+          k0, K, tid);
     } else {
-      const int kp = k0 + WLoad::part(tid) * WLoad::EPT;
-      bw.load([&](int i) { return w + int64_t(kp + i < K ? kp + i : K - 1) * N + n0; }, WLoad::col(tid), N - n0);
+      bw.load(
+          [&](int i) {
+            const int k = WTile::step(i, tid), left = K - k0;
+            return w + (int64_t(k0) * N + n0) + (k < left ? k : left - 1) * N;
+          },
+          N - n0, tid);
     }
   };
   f32x4 acc[MI][NI];
@@ -538,19 +555,25 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int wm = 64 * (wave % 2), wn = TN / 2 * (wave / 2);
+  const typename XTile::Reader x_read(wm / 16, l);
+  const typename WTile::Reader w_read(wn / 16, l);
   const float xs = (tid / 8) % 2 ? -kScale : kScale;  // odd rows negated
   load(0);
   for (int k0 = 0; k0 < K; k0 += KS) {
     lds_sync<4>();  // the previous step has been read
-    a.template put<R, false>(lds, 0, g.act, xs, k0, K, tid);
-    if constexpr (WT)
-      bw.template put<R, !F32>(lds, kTileRows, false, kScale, k0, K, tid);
-    else
-      bw.template put<R, !F32>(lds, kTileRows, false, kScale,
-                               steps_below(k0 + WLoad::part(tid) * WLoad::EPT, K, WLoad::EPT), tid);
+    a.put(x_lds, !WT && g.act, xs, k0, K, tid);
+    if constexpr (WT) {
+      bw.put(w_lds, false, kScale, k0, K, tid);
+    } else {
+      if (k0 + KS > K) {
+#pragma unroll
+        for (int i = 0; i < WTile::NP; ++i) missing |= (k0 + WTile::step(i, tid) >= K) << i;
+      }
+      bw.put(w_lds, false, kScale, N - n0, missing, tid);
+    }
     lds_sync<4>();
     if (k0 + KS < K) load(k0 + KS);
-    multiply<T, R, MI, NI>(lds, wm, kTileRows + wn, 1.f, acc, l);
+    multiply<T, XTile, WTile>(x_lds, w_lds, x_read, w_read, 1.f, acc);
   }
   if constexpr (F32) {
     if (any_not_finite(acc)) {
@@ -562,8 +585,8 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
             return g.act ? silu(v) : v;
           },
           [&](int j, int64_t k) {
-            const int n = n0 + wn + 16 * j + l % 16;
-            return n >= N ? 0.f : WT ? w[int64_t(n - n0) * K + k] : w[k * N + n];
+            const int n = n0 + wn + 16 * j + l % 16;  // fp32: columns in order
+            return n >= N ? 0.f : WT ? w[int64_t(n) * K + k] : w[k * N + n];
           });
     } else {
       const float u = l % 2 ? -kUnscale : kUnscale;
@@ -586,13 +609,269 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
       float v[W];
 #pragma unroll
       for (int e = 0; e < W; ++e) v[e] = acc[i][j + e / 4][e % 4];
-      if (pre) {
-        float p[W];
-        load_row<W>(pre + int64_t(r) * g.ldp + n, p, N - n);
+      if (WT && pre) {
+        const u32x4 p = load_bits<W>(pre + int64_t(r) * g.ldp + n, N - n);
 #pragma unroll
-        for (int e = 0; e < W; ++e) v[e] *= silu_grad(p[e]);
+        for (int e = 0; e < W; ++e) v[e] *= silu_grad(value_of<T>(p, e));
       }
       store_row<W>(y + int64_t(r) * g.ldy + n, v, N - n);
+    }
+  }
+}
+
+// The fp32 products where the weights of a group fit the LDS and there are many
+// rows: a workgroup of 8 waves holds the split form of one group's W (TN columns)
+// and streams rows past it.  X goes from memory straight to the matrix
+// instructions' operand registers (lane l has row l % 16 and 8 consecutive values
+// from 8 (l / 16) on), so each value is read and split once, and waves meet at no
+// barrier but when the group changes.  A wave goes through (32 rows, step) pairs
+// with loads two steps ahead, also from one 32 rows to the next.
+constexpr int kStreamThreads = 512, kStreamWaves = kStreamThreads / kWave, kStreamLds = 147456;
+constexpr int kStreamGroups = 256;  // workgroups: one on every compute unit
+
+template <int TN>
+constexpr int stream_k() {  // the longest contraction whose weights fit: whole pairs of steps
+  return kStreamLds / (Kind<float>::P * TN * 128) * 64;
+}
+
+template <int TN, bool WT>
+__global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(ProductArgs g) {
+  constexpr int KS = Kind<float>::KS, PE = Kind<float>::PE, XP = 8 / PE, MT = 2, NI = TN / 16, RB = 16 * MT;
+  using WTile = std::conditional_t<WT, Along<float, TN, false>, Across<float, TN, false>>;
+  __shared__ u32x4 w_lds[kStreamLds / 16];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
+  const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
+  const int64_t share = b / g.nt;
+  const int n0 = int(b % g.nt) * TN, K = g.K, N = g.N, steps = (K + 2 * KS - 1) / (2 * KS) * 2;  // an even number
+  const float *x = static_cast<const float *>(g.x);
+  float *y = static_cast<float *>(g.y);
+  const float *pre = static_cast<const float *>(g.pre);
+  const float xs = l % 2 ? -kScale : kScale;  // odd rows negated
+  const typename WTile::Reader w_read(0, l);
+  // Shares of equal cost: a group costs its rows and what it takes to load its
+  // weights and to fill the waves, kGroupRows rows.  Cost units a of group g lie at
+  // its rows from offsets[g] + kGroupRows (g + 1) on.
+  constexpr int64_t kGroupRows = kStreamWaves * RB;
+  const int64_t units = g.M + kGroupRows * (g.G + 1), stop = units * (share + 1) / g.mt;
+  for (int64_t unit = units * share / g.mt; unit < stop;) {
+    int lg = l;
+    asm volatile("" : "+v"(lg));  // addresses of a group are formed in its turn
+    const Tile t = find_group(g.offsets, g.G, g.M, unit, kGroupRows, lg);
+    const int64_t first = t.begin + kGroupRows * (t.g + 1);  // the unit of the group's first row
+    const int64_t lo = t.begin + (unit > first ? unit - first : 0);
+    const int64_t hi = t.end < t.begin + stop - first ? t.end : t.begin + stop - first;
+    const int64_t next_group = first + (t.end - t.begin);
+    if (next_group <= unit) break;  // offsets out of order
+    unit = next_group;
+    if (lo >= hi) continue;
+    const int chunks = int((hi - lo + RB - 1) / RB);
+    // lane i: row i of the 32 rows of chunk c, -1 past the end or out of range
+    auto list = [&](int c) -> int {
+      const int64_t at = lo + int64_t(c) * RB + lg % RB, in = at < hi ? at : hi - 1;
+      const int r = g.rows ? g.rows[in] : int(in);
+      return at < hi && r >= 0 && r < g.M ? r : -1;
+    };
+    auto row_of = [&](int rows, int i) { return __shfl(rows, 16 * i + l % 16); };
+    if (t.g == g.G) {  // no type
+      for (int c = wave; c < chunks; c += kStreamWaves) {
+        const int rows = list(c);
+        for (int i = 0; i < RB; ++i) {
+          const int r = __builtin_amdgcn_readlane(rows, i);
+          if (r < 0) continue;
+          for (int n = n0 + l; n < N && n < n0 + TN; n += kWave) y[int64_t(r) * g.ldy + n] = 0.f;
+        }
+      }
+      continue;
+    }
+    const float *w = static_cast<const float *>(g.w) + int64_t(t.g) * K * N;
+    __syncthreads();  // the group before has been multiplied
+    // each half of the workgroup fills every other tile
+    const int ft = wave % 4 * kWave + lg;
+    const int half = tid / kThreads;
+    auto fill_load = [&](WTile &f, int tile) {
+      const int k0 = tile * KS;
+      if constexpr (WT) {
+        f.load(
+            [&](int i) {
+              const int n = ft / 8 + 32 * i;  // columns past the last read it, and reach no output
+              return w + int64_t(n0) * K + (n < N - n0 ? n : N - n0 - 1) * K;
+            },
+            k0, K, ft);
+      } else {
+        f.load(
+            [&](int i) {
+              const int k = WTile::step(i, ft), left = K - k0;
+              return w + (int64_t(k0) * N + n0) + (k < left ? k : left - 1) * N;
+            },
+            N - n0, ft);
+      }
+    };
+    auto fill_put = [&](WTile &f, int tile) {
+      const int k0 = tile * KS;
+      if constexpr (WT) {
+        f.put(w_lds + tile * WTile::SIZE, false, kScale, k0, K, ft);
+      } else {
+        int missing = 0;
+#pragma unroll
+        for (int i = 0; i < WTile::NP; ++i) missing |= (k0 + WTile::step(i, ft) >= K) << i;
+        f.put(w_lds + tile * WTile::SIZE, false, kScale, N - n0, missing, ft);
+      }
+    };
+#pragma unroll 1
+    for (int tile = half; tile < steps; tile += 2) {
+      WTile f;
+      fill_load(f, tile);
+      fill_put(f, tile);
+    }
+    __syncthreads();
+    if (wave < chunks) {
+      // the loads' side: chunk lc, step lk; next: the rows of the chunk after lc
+      int lc = wave, lk = 0, next = list(lc);
+      const float *xp[MT];
+      auto point = [&]() {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int r = row_of(next, i);
+          xp[i] = x + (r < 0 ? 0 : int64_t(r) * g.ldx);
+        }
+        next = list(lc + kStreamWaves);
+      };
+      point();
+      auto load = [&](u32x4 (&v)[MT][XP]) {
+        const int k = lk * 32 + 8 * (l / 16);
+#pragma unroll
+        for (int q = 0; q < XP; ++q) {
+          const unsigned at = unsigned(k + PE * q < K - PE ? k + PE * q : K - PE);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) v[i][q] = *reinterpret_cast<const u32x4_any *>(xp[i] + at);
+        }
+        if (++lk == steps) {
+          lk = 0;
+          lc += kStreamWaves;
+          point();
+        }
+      };
+      f32x4 acc[MT][NI];
+      auto clear = [&]() {
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      };
+      clear();
+      int cc = wave, ck = 0, rows = list(cc);  // the products' side
+      auto step = [&](u32x4 (&v)[MT][XP]) {
+        bf16x8 xf[MT][3];
+        const int k = ck * 32 + 8 * (l / 16);
+        if (ck * 32 + 32 > K) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int q = 0; q < XP; ++q) v[i][q] = shifted<float>(v[i][q], shift_of<float>(k + PE * q, K));
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          u32x2 o[2][3];
+          split_piece(v[i][0], !WT && g.act, xs, o[0]);
+          split_piece(v[i][1], !WT && g.act, xs, o[1]);
+#pragma unroll
+          for (int p = 0; p < 3; ++p)
+            xf[i][p] = __builtin_bit_cast(bf16x8, u32x4{o[0][p][0], o[0][p][1], o[1][p][0], o[1][p][1]});
+        }
+        load(v);
+        const u32x4 *d = w_lds + ck * WTile::SIZE;
+        typename WTile::Reader read = w_read;
+        if constexpr (!WT) asm volatile("" : "+v"(read.base));  // one register, not one for each j
+        auto frag = [&](int p, int j) { return read.get(d, p, j, 0); };
+        constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};
+#pragma unroll
+        for (int j = 0; j < NI; ++j) {
+          if (j % 2 == 0) __builtin_amdgcn_sched_barrier(0);  // operands of two products at a time
+          bf16x8 a[3];
+          f32x4 sum[MT];
+#pragma unroll
+          for (int p = 0; p < 3; ++p) a[p] = frag(p, j);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) sum[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int q = 0; q < 6; ++q)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) sum[i] = mfma16(a[PA[q]], xf[i][PB[q]], sum[i]);
+#pragma unroll
+          for (int i = 0; i < MT; ++i) acc[i][j] += sum[i];
+        }
+        ++ck;
+      };
+      // writes the rows of a chunk
+      auto finish = [&]() {
+        int lane = l;
+        asm volatile("" : "+v"(lane));  // keeps the addresses formed here out of the loop's registers
+        if (any_not_finite(acc)) {
+          int row[MT];
+#pragma unroll
+          for (int i = 0; i < MT; ++i) row[i] = row_of(rows, i);
+          multiply_again(
+              acc, K, lane,
+              [&](int i, int64_t k) {
+                const float a = row[i] < 0 ? 0.f : x[int64_t(row[i]) * g.ldx + k];
+                return !WT && g.act ? silu(a) : a;
+              },
+              [&](int j, int64_t k) {
+                const int n = n0 + 16 * j + lane % 16;
+                return n >= N ? 0.f : WT ? w[int64_t(n) * K + k] : w[k * N + n];
+              });
+        } else {
+          const float u = l % 2 ? -kUnscale : kUnscale;
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] *= u;
+        }
+        constexpr int W = 4;
+        int row[MT];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) row[i] = row_of(rows, i);
+        const int n = n0 + W * (lane / 16);
+        if (WT && pre) {
+          const bool whole = N - n0 >= TN;
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            const float *p = pre + int64_t(row[i] < 0 ? 0 : row[i]) * g.ldp + n;
+            __builtin_amdgcn_sched_barrier(0);  // one row's values at a time
+            u32x4 v[NI];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) v[j] = load_bits<W>(p + 16 * j, whole ? W : N - n - 16 * j);
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j][e] *= silu_grad(value_of<float>(v[j], e));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          if (row[i] < 0) continue;
+          float *o = y + int64_t(row[i]) * g.ldy + n;
+#pragma unroll
+          for (int j = 0; j < NI; ++j) {
+            const float v[W] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            store_row<W>(o + 16 * j, v, N - n - 16 * j);
+          }
+        }
+        clear();
+        ck = 0;
+        cc += kStreamWaves;
+        rows = list(cc);
+      };
+      u32x4 v0[MT][XP], v1[MT][XP];
+      load(v0);
+      load(v1);
+      while (cc < chunks) {
+        for (int k = 0; k < steps; k += 2) {
+          step(v0);
+          step(v1);
+        }
+        finish();
+      }
     }
   }
 }
@@ -618,13 +897,17 @@ struct WeightArgs {
 // group has more than 1 << shift rows, so the next one's slots start behind it.
 template <class T, int TK, int TN>
 __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
-  constexpr int P = Kind<T>::P, KS = Kind<T>::KS, R = TK + TN, C = KS / 8;
+  constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int MI = TK / 32, NI = TN / 32;
-  __shared__ u32x4 lds[P * R * C];
+  using XTile = Across<T, TK, false>;
+  using YTile = Across<T, TN, false>;
+  __shared__ u32x4 x_lds[XTile::SIZE], y_lds[YTile::SIZE];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int tiles = g.kt * g.nt;
-  const int64_t b = xcd_order(blockIdx.x, g.ranges * tiles);
+  // in plain order over the XCDs: groups differ in length, and a range's tiles
+  // take the same time
+  const int64_t b = blockIdx.x;
   const Tile t = find_tile(g.offsets, g.G, g.M, g.shift, b / tiles, l);
   if (t.g == g.G) return;
   const int64_t begin = t.begin;
@@ -633,24 +916,29 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
   const int64_t end = t.m0 + (int64_t(1) << g.shift) < t.end ? t.m0 + (int64_t(1) << g.shift) : t.end;
   const int k0 = int(b % tiles) / g.nt * TK, n0 = int(b % tiles) % g.nt * TN, K = g.K, N = g.N;
   const T *x = static_cast<const T *>(g.x), *dy = static_cast<const T *>(g.dy);
-  using XLoad = Across<T, TK>;
-  using YLoad = Across<T, TN>;
-  XLoad xa;
-  YLoad ya;
   auto row_of = [&](int64_t i) -> int {
     if (i >= end) return -1;
     const int64_t r = g.rows ? int64_t(g.rows[i]) : i;
     return r < 0 || r >= g.M ? -1 : int(r);
   };
-  // the rows of a step are the same for all lanes: lane i loads row i of the step
-  // two ahead, the addresses are formed with its value in a scalar register
-  const int xpart = XLoad::part(tid) * XLoad::EPT, ypart = YLoad::part(tid) * YLoad::EPT;
-  auto load = [&](int rows) {
-    const int r = rows < 0 ? 0 : rows;
-    xa.load([&](int i) { return x + int64_t(__builtin_amdgcn_readlane(r, xpart + i)) * g.ldx + k0; }, XLoad::col(tid),
-            K - k0);
-    ya.load([&](int i) { return dy + int64_t(__builtin_amdgcn_readlane(r, ypart + i)) * g.lddy + n0; },
-            YLoad::col(tid), N - n0);
+  XTile xa;
+  YTile ya;
+  // list entries of the next step, loaded a step ahead; bit i of missing: none
+  int xr[XTile::NP], yr[YTile::NP], xm = 0, ym = 0;
+  auto list = [&](int64_t m) {
+#pragma unroll
+    for (int i = 0; i < XTile::NP; ++i) xr[i] = row_of(m + XTile::step(i, tid));
+#pragma unroll
+    for (int i = 0; i < YTile::NP; ++i) yr[i] = TK == TN ? xr[i < XTile::NP ? i : 0] : row_of(m + YTile::step(i, tid));
+  };
+  auto load = [&]() {
+    xm = ym = 0;
+#pragma unroll
+    for (int i = 0; i < XTile::NP; ++i) xm |= int(xr[i] < 0) << i;
+#pragma unroll
+    for (int i = 0; i < YTile::NP; ++i) ym |= int(yr[i] < 0) << i;
+    xa.load([&](int i) { return x + k0 + (xr[i] < 0 ? 0 : int64_t(xr[i]) * g.ldx); }, K - k0, tid);
+    ya.load([&](int i) { return dy + n0 + (yr[i] < 0 ? 0 : int64_t(yr[i]) * g.lddy); }, N - n0, tid);
   };
   f32x4 acc[MI][NI];
 #pragma unroll
@@ -658,23 +946,24 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   const int wk = TK / 2 * (wave % 2), wn = TN / 2 * (wave / 2);
+  const typename XTile::Reader x_read(wk / 16, l);
+  const typename YTile::Reader y_read(wn / 16, l);
   float sign = 1.f;
-  const int lk = l % KS;
-  int rows = row_of(t.m0 + lk);
-  uint64_t valid = __ballot(rows >= 0);
-  if (t.m0 < end) load(rows);
-  rows = row_of(t.m0 + KS + lk);
+  if (t.m0 < end) {
+    list(t.m0);
+    load();
+    list(t.m0 + KS);
+  }
   for (int64_t m = t.m0; m < end; m += KS) {
     lds_sync<4>();
-    xa.template put<R, false>(lds, 0, g.act, sign * kScale, uint32_t(valid >> xpart) & steps_below(0, KS, XLoad::EPT), tid);
-    ya.template put<R, false>(lds, TK, false, kScale, uint32_t(valid >> ypart) & steps_below(0, KS, YLoad::EPT), tid);
+    xa.put(x_lds, g.act, sign * kScale, K - k0, xm, tid);
+    ya.put(y_lds, false, kScale, N - n0, ym, tid);
     lds_sync<4>();
-    valid = __ballot(rows >= 0);
     if (m + KS < end) {
-      load(rows);
-      rows = row_of(m + 2 * KS + lk);
+      load();
+      list(m + 2 * KS);
     }
-    multiply<T, R, MI, NI>(lds, wk, TK + wn, sign, acc, l);
+    multiply<T, XTile, YTile>(x_lds, y_lds, x_read, y_read, sign, acc);
     sign = -sign;
   }
   if constexpr (F32) {
@@ -793,8 +1082,9 @@ struct ProductF8Args {
 // below the bf16 output's 2^-8, and the reason that there is no fp32 output.
 template <int TN>
 __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g) {
-  constexpr int KS = 128, C = KS / 16, R = kTileRows + TN, MI = 4, NI = TN / 32;
-  __shared__ u32x4 lds[R * C];
+  constexpr int KS = 128, MI = 4, NI = TN / 32;
+  auto chunk_at = [](int r, int c) { return swizzled<KS / 16>(r, c); };
+  __shared__ u32x4 x_lds[kTileRows * KS / 16], w_lds[TN * KS / 16];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
@@ -883,25 +1173,25 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
       for (int i = 0; i < NW; ++i) bw[i] = cut(bw[i], k);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) lds[chunk_at<C, R>(0, tid / 8 + 32 * i, tid % 8)] = a[i];
+    for (int i = 0; i < 4; ++i) x_lds[chunk_at(tid / 8 + 32 * i, tid % 8)] = a[i];
 #pragma unroll
-    for (int i = 0; i < NW; ++i) lds[chunk_at<C, R>(0, kTileRows + slot_of<true>(tid / 8 + 32 * i), tid % 8)] = bw[i];
+    for (int i = 0; i < NW; ++i) w_lds[chunk_at(tid / 8 + 32 * i, tid % 8)] = bw[i];
     lds_sync<4>();
     float sc[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) sc[i] = sx[i] * sw;
     if (k0 + KS < K) load(k0 + KS);
     // lane l takes chunks l / 16 and l / 16 + 4 of both operands
-    auto frag = [&](int r) {
-      const u32x4 lo = lds[chunk_at<C, R>(0, r, l / 16)], hi = lds[chunk_at<C, R>(0, r, l / 16 + 4)];
+    auto frag = [&](const u32x4 *lds, int r) {
+      const u32x4 lo = lds[chunk_at(r, l / 16)], hi = lds[chunk_at(r, l / 16 + 4)];
       return i32x8{int(lo[0]), int(lo[1]), int(lo[2]), int(lo[3]), int(hi[0]), int(hi[1]), int(hi[2]), int(hi[3])};
     };
     i32x8 xf[MI];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) xf[i] = frag(wm + 16 * i + l % 16);
+    for (int i = 0; i < MI; ++i) xf[i] = frag(x_lds, wm + 16 * i + l % 16);
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const i32x8 wf = frag(kTileRows + wn + 16 * j + l % 16);
+      const i32x8 wf = frag(w_lds, wn + column_of<true>(j, l % 16));
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
@@ -933,6 +1223,23 @@ template <class T, bool WT>
 void launch_product(ProductArgs g, hipStream_t s) {
   const bool narrow = g.N <= 64;
   g.nt = narrow ? 1 : int(cdiv(g.N, 128));
+  if constexpr (sizeof(T) == 4) {
+    // Rows past stationary weights, or tiles.  Tiles against this, us, forward, 1 and
+    // 100 types: M = 32,000 K = 128 N = 128 18 against 21 and 22 against 24;
+    // M = 128,000 44 against 38 and 52 against 43; M = 500,000 168 against 138 and
+    // 178 against 140 (K = 192: 220 against 183); with few rows to a type the
+    // weights' loads tell: M = 8,000 and 100 types 17 against 37.
+    const int fits = narrow ? stream_k<64>() : stream_k<128>();
+    if (g.K >= Kind<T>::PE && g.K <= fits && g.M >= 65536 && g.M >= 512 * int64_t(g.G)) {
+      g.mt = std::max(1, kStreamGroups / g.nt);
+      const dim3 grid(unsigned(g.mt * g.nt)), block(kStreamThreads);
+      if (narrow)
+        hipLaunchKernelGGL((product_stream_kernel<64, WT>), grid, block, 0, s, g);
+      else
+        hipLaunchKernelGGL((product_stream_kernel<128, WT>), grid, block, 0, s, g);
+      return;
+    }
+  }
   g.mt = tile_bound(g.M, g.G, kTileShift);
   const dim3 grid(unsigned(g.mt * g.nt)), block(kThreads);
   if (narrow)
@@ -952,7 +1259,7 @@ WeightShape weight_shape(int64_t M, int K, int N) {
   // about 768 workgroups, ranges of at least 256 rows
   const int64_t rows = M * z.kt * z.nt / 768;
   z.shift = 8;
-  while ((int64_t(1) << z.shift) < rows && z.shift < 30) ++z.shift;
+  while (3 * (int64_t(1) << z.shift) < 2 * rows && z.shift < 30) ++z.shift;
   z.slot = cdiv(int64_t(K) * N, 4) * 4;
   z.slots = M > (int64_t(1) << z.shift) ? 2 * (M >> z.shift) + 1 : 0;
   return z;

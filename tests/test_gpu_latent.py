@@ -180,6 +180,38 @@ def test_products_over_many_rows(at, dtype, m, k, n, g):
     _product_case(at, m, k, n, g, dtype, True)
 
 
+@pytest.mark.parametrize("m,k,n,g,act", [(66003, 192, 128, 3, False), (70000, 128, 64, 100, True), (65600, 20, 130, 16, True),
+                                         (65536, 65, 191, 5, False), (90001, 4, 3, 128, False), (65537, 384, 61, 2, True)])
+def test_products_of_many_rows(at, m, k, n, g, act):
+    """fp32 rows that are streamed past stationary weights, with rows of no type and types of few rows."""
+    _note(f"[gpu] product M={m} K={k} N={n} G={g} f32 streamed")
+    _product_case(at, m, k, n, g, F32, act)
+
+
+def test_products_of_many_rows_special_values(at):
+    gen = _gen(13)
+    m, k, n = 66000, 72, 70
+    x, w, dy = _normal(gen, m, k), _normal(gen, 2, k, n), _normal(gen, m, n)
+    x[3, 5], x[40000, 69], x[40031, 0], x[65999, 7] = float("inf"), float("nan"), float("-inf"), 3e38
+    t = torch.randint(-1, 2, (m,), generator=gen, dtype=torch.int32)
+    t[[3, 40000, 40031, 65999]] = 1
+    offsets, rows = at.allegro_group_rows(t.to(DEV), 2)
+    y = _f64(at.allegro_grouped_matmul(x.to(DEV), w.to(DEV), offsets, rows))
+    ref = ol.grouped_matmul(t.numpy(), _f64(x), _f64(w), False)
+    over = np.abs(ref) > 3.5e38  # beyond fp32
+    assert np.array_equal(np.isnan(y), np.isnan(ref))
+    assert np.array_equal(y[np.isinf(ref)], ref[np.isinf(ref)]) and np.all(np.isinf(y[over & np.isfinite(ref)]))
+    ordinary = np.ones(m, bool)
+    ordinary[[3, 40000, 40031, 65999]] = False
+    assert np.max(np.abs(y - ref)[ordinary]) <= 1e-4
+    # many rows whose list is out of order or range
+    for off in ([0, 50000, 100], [-5, 1 << 40, 20], [m, 0, 0]):
+        bad = torch.randint(-1000, 2 * m, (m,), generator=gen, dtype=torch.int32).to(DEV)
+        at.allegro_grouped_matmul(x.to(DEV), w.to(DEV), torch.tensor(off, device=DEV), bad)
+        at.allegro_grouped_matmul_backward(x.to(DEV), w.to(DEV), dy.to(DEV), torch.tensor(off, device=DEV), bad)
+    torch.cuda.synchronize()
+
+
 def test_products_without_any_row(at):
     for dtype in (F32, BF16):
         x, w = torch.empty(0, 12, dtype=dtype, device=DEV), torch.randn(3, 12, 20, device=DEV).to(dtype)
