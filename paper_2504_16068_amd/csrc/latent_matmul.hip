@@ -209,10 +209,15 @@ __device__ __forceinline__ u32x4 shifted(u32x4 a, int by) {
   return a;
 }
 
-// 16-byte chunk c of row r of rows of 4 or 8 chunks (64 or 128 bytes).
-template <int C>
+// 16-byte chunk c of row r of rows of 4 or 8 chunks (64 or 128 bytes).  One chunk
+// of the rows that 8 or 16 consecutive lanes read lies in distinct banks: of
+// consecutive rows, or (WIDE) of those that column_of<true> picks.
+template <int C, bool WIDE>
 __device__ __forceinline__ int swizzled(int r, int c) {
-  return r * C + (c ^ (C == 4 ? ((r >> 1) & 3) ^ ((r >> 3) & 1) : (r & 7) ^ ((r >> 3) & 1)));
+  const int f = C == 4 ? ((r >> 1) & 3) ^ ((r >> 3) & 1)
+                : WIDE ? ((r & 3) | (r >> 1 & 4)) ^ ((r >> 4) & 1)
+                       : (r & 7) ^ ((r >> 3) & 1);
+  return r * C + (c ^ f);
 }
 
 // A tile of `ROWS` rows (of X, or columns of the result) whose contraction runs
@@ -235,7 +240,8 @@ struct Along {
       for (int i = 0; i < NP; ++i) v[i] = shifted<T>(v[i], shift_of<T>(k0 + PE * (tid % 8), n));
     }
     // rows 32 apart are swizzled alike
-    const int at = P == 3 ? 2 * swizzled<C>(tid / 8, tid % 8 / 2) + tid % 2 : swizzled<C>(tid / 8, tid % 8);
+    const int at =
+        P == 3 ? 2 * swizzled<C, WIDE>(tid / 8, tid % 8 / 2) + tid % 2 : swizzled<C, WIDE>(tid / 8, tid % 8);
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
       if constexpr (P == 3) {
@@ -256,7 +262,7 @@ struct Along {
     int base[WIDE ? 2 : 1];
     __device__ __forceinline__ Reader(int j0, int l) {
 #pragma unroll
-      for (int h = 0; h < (WIDE ? 2 : 1); ++h) base[h] = swizzled<C>(column_of<WIDE>(j0 + h, l % 16), l / 16);
+      for (int h = 0; h < (WIDE ? 2 : 1); ++h) base[h] = swizzled<C, WIDE>(column_of<WIDE>(j0 + h, l % 16), l / 16);
     }
     __device__ __forceinline__ bf16x8 get(const u32x4 *lds, int p, int j, int kk) const {
       const int row = p * ROWS + (WIDE ? 32 * (j / 2) : 16 * j);
@@ -435,6 +441,15 @@ __device__ __forceinline__ void store_row(uint16_t *p, const float *v, int left)
       if (i < left) p[i] = bf16_bits(v[i]);
   }
 }
+__device__ __forceinline__ void store_bits(uint16_t *p, u32x4 v, int left) {
+  if (left >= 8) {
+    *reinterpret_cast<u32x4_any *>(p) = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 7; ++i)
+      if (i < left) p[i] = uint16_t(v[i / 2] >> (16 * (i % 2)));
+  }
+}
 template <int W, class T>  // 16 bytes in both types
 __device__ __forceinline__ u32x4 load_bits(const T *p, int left) {
   if (left >= W) return *reinterpret_cast<const u32x4_any *>(p);
@@ -458,6 +473,27 @@ __device__ __forceinline__ float value_of(u32x4 v, int e) {
     const uint32_t bits = e % 2 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16;
     return __builtin_bit_cast(float, bits);
   }
+}
+
+// Lanes 4 a + b (b < 4) hold, in v[0 .. 3], 16 bytes of each of four columns' parts
+// of a row of their own; afterwards lane b holds part b of the four rows, v[s]
+// that of lane 4 a + s.
+__device__ __forceinline__ void quad_transpose(u32x4 (&v)[4], int l) {
+  auto swap = [&](u32x4 &lo, u32x4 &hi, auto perm, bool upper) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t a = lo[e], b = hi[e];
+      const uint32_t got = uint32_t(__builtin_amdgcn_mov_dpp(int(upper ? a : b), perm(), 0xf, 0xf, true));
+      lo[e] = upper ? got : a;
+      hi[e] = upper ? b : got;
+    }
+  };
+  const std::integral_constant<int, 0xb1> by1;  // lanes 1, 0, 3, 2 of every four
+  const std::integral_constant<int, 0x4e> by2;  // lanes 2, 3, 0, 1
+  swap(v[0], v[1], by1, l & 1);
+  swap(v[2], v[3], by1, l & 1);
+  swap(v[0], v[2], by2, l & 2);
+  swap(v[1], v[3], by2, l & 2);
 }
 
 // Row list of a tile: srow[i] = row of list position m0 + i, -1 past the end or
@@ -634,6 +670,49 @@ constexpr int stream_k() {  // the longest contraction whose weights fit: whole 
   return kStreamLds / (Kind<float>::P * TN * 128) * 64;
 }
 
+// Goes through share `share` of `shares` of equal cost: a group costs its rows and
+// what it takes to load its weights and to fill the waves, as much as RB rows for
+// each wave.  Calls group(g, chunks, list) for its part of each group, g == G for
+// the rows without a type; list(c) gives lane i row i of the RB rows of chunk c, -1
+// past the end or out of range.  Every wave of the workgroup makes the same calls.
+template <int RB, class Group>
+__device__ __forceinline__ void stream_share(const int64_t *__restrict__ offsets, const int32_t *__restrict__ rows, int G,
+                                             int64_t M, int64_t share, int64_t shares, int l, Group group) {
+  // cost units of group g lie at its rows from offsets[g] + kGroupRows (g + 1) on
+  constexpr int64_t kGroupRows = kStreamWaves * RB;
+  const int64_t units = M + kGroupRows * (G + 1), stop = units * (share + 1) / shares;
+  for (int64_t unit = units * share / shares; unit < stop;) {
+    int lg = l;
+    asm volatile("" : "+v"(lg));  // addresses of a group are formed in its turn
+    const Tile t = offsets ? find_group(offsets, G, M, unit, kGroupRows, lg) : Tile{0, 0, 0, M};
+    const int64_t first = t.begin + kGroupRows * (t.g + 1);  // the unit of the group's first row
+    const int64_t lo = t.begin + (unit > first ? unit - first : 0);
+    const int64_t hi = t.end < t.begin + stop - first ? t.end : t.begin + stop - first;
+    const int64_t next_group = first + (t.end - t.begin);
+    if (next_group <= unit) break;  // offsets out of order, or no more groups
+    unit = next_group;
+    if (lo >= hi) continue;
+    group(t.g, int((hi - lo + RB - 1) / RB), [=](int c) -> int {
+      const int64_t at = lo + int64_t(c) * RB + lg % RB, in = at < hi ? at : hi - 1;
+      const int r = rows ? rows[in] : int(in);
+      return at < hi && r >= 0 && r < M ? r : -1;
+    });
+  }
+}
+
+// Zeros for columns n0 .. n1 - 1 of the wave's share of the rows without a type.
+template <int RB, class T, class List>
+__device__ __forceinline__ void stream_zeros(int chunks, List list, T *y, int64_t ldy, int n0, int n1, int wave, int l) {
+  for (int c = wave; c < chunks; c += kStreamWaves) {
+    const int rows = list(c);
+    for (int i = 0; i < RB; ++i) {
+      const int r = __builtin_amdgcn_readlane(rows, i);
+      if (r < 0) continue;
+      for (int n = n0 + l; n < n1; n += kWave) y[int64_t(r) * ldy + n] = T(0);
+    }
+  }
+}
+
 template <int TN, bool WT>
 __global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(ProductArgs g) {
   constexpr int KS = Kind<float>::KS, PE = Kind<float>::PE, XP = 8 / PE, MT = 2, NI = TN / 16, RB = 16 * MT;
@@ -641,49 +720,21 @@ __global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(Produ
   __shared__ u32x4 w_lds[kStreamLds / 16];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
-  const int64_t share = b / g.nt;
   const int n0 = int(b % g.nt) * TN, K = g.K, N = g.N, steps = (K + 2 * KS - 1) / (2 * KS) * 2;  // an even number
   const float *x = static_cast<const float *>(g.x);
   float *y = static_cast<float *>(g.y);
   const float *pre = static_cast<const float *>(g.pre);
   const float xs = l % 2 ? -kScale : kScale;  // odd rows negated
   const typename WTile::Reader w_read(0, l);
-  // Shares of equal cost: a group costs its rows and what it takes to load its
-  // weights and to fill the waves, kGroupRows rows.  Cost units a of group g lie at
-  // its rows from offsets[g] + kGroupRows (g + 1) on.
-  constexpr int64_t kGroupRows = kStreamWaves * RB;
-  const int64_t units = g.M + kGroupRows * (g.G + 1), stop = units * (share + 1) / g.mt;
-  for (int64_t unit = units * share / g.mt; unit < stop;) {
-    int lg = l;
-    asm volatile("" : "+v"(lg));  // addresses of a group are formed in its turn
-    const Tile t = find_group(g.offsets, g.G, g.M, unit, kGroupRows, lg);
-    const int64_t first = t.begin + kGroupRows * (t.g + 1);  // the unit of the group's first row
-    const int64_t lo = t.begin + (unit > first ? unit - first : 0);
-    const int64_t hi = t.end < t.begin + stop - first ? t.end : t.begin + stop - first;
-    const int64_t next_group = first + (t.end - t.begin);
-    if (next_group <= unit) break;  // offsets out of order
-    unit = next_group;
-    if (lo >= hi) continue;
-    const int chunks = int((hi - lo + RB - 1) / RB);
-    // lane i: row i of the 32 rows of chunk c, -1 past the end or out of range
-    auto list = [&](int c) -> int {
-      const int64_t at = lo + int64_t(c) * RB + lg % RB, in = at < hi ? at : hi - 1;
-      const int r = g.rows ? g.rows[in] : int(in);
-      return at < hi && r >= 0 && r < g.M ? r : -1;
-    };
-    auto row_of = [&](int rows, int i) { return __shfl(rows, 16 * i + l % 16); };
-    if (t.g == g.G) {  // no type
-      for (int c = wave; c < chunks; c += kStreamWaves) {
-        const int rows = list(c);
-        for (int i = 0; i < RB; ++i) {
-          const int r = __builtin_amdgcn_readlane(rows, i);
-          if (r < 0) continue;
-          for (int n = n0 + l; n < N && n < n0 + TN; n += kWave) y[int64_t(r) * g.ldy + n] = 0.f;
-        }
-      }
-      continue;
+  stream_share<RB>(g.offsets, g.rows, g.G, g.M, b / g.nt, g.mt, l, [&](int group, int chunks, auto list) {
+    if (group == g.G) {
+      stream_zeros<RB>(chunks, list, y, g.ldy, n0, n0 + TN < N ? n0 + TN : N, wave, l);
+      return;
     }
-    const float *w = static_cast<const float *>(g.w) + int64_t(t.g) * K * N;
+    auto row_of = [&](int rows, int i) { return __shfl(rows, 16 * i + l % 16); };
+    int lg = l;
+    asm volatile("" : "+v"(lg));
+    const float *w = static_cast<const float *>(g.w) + int64_t(group) * K * N;
     __syncthreads();  // the group before has been multiplied
     // each half of the workgroup fills every other tile
     const int ft = wave % 4 * kWave + lg;
@@ -873,7 +924,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(Produ
         finish();
       }
     }
-  }
+  });
 }
 
 // ------------------------------------------------------- weight gradient
@@ -1074,6 +1125,27 @@ struct ProductF8Args {
   int64_t mt;
 };
 
+// Drops the first `by` bytes of 16; zeros follow the last.
+__device__ __forceinline__ u32x4 cut_bytes(u32x4 a, int by) {
+  u32x4 o;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_alignbit(i < 3 ? a[i + 1] : 0u, a[i], 8 * (by % 4));
+  if (by & 4) o = u32x4{o[1], o[2], o[3], 0};
+  if (by & 8) o = u32x4{o[2], o[3], 0, 0};
+  if (by >= 16) o = u32x4{0, 0, 0, 0};
+  return o;
+}
+
+__device__ __forceinline__ i32x8 operand_f8(u32x4 lo, u32x4 hi) {
+  return i32x8{int(lo[0]), int(lo[1]), int(lo[2]), int(lo[3]), int(hi[0]), int(hi[1]), int(hi[2]), int(hi[3])};
+}
+
+// The sums of one block of 128; both block scales of the instruction are 2^(127 - 127).
+__device__ __forceinline__ f32x4 block_sum_f8(i32x8 w, i32x8 x) {
+  return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(w, x, f32x4{0.f, 0.f, 0.f, 0.f}, 0, 0, 0, 0x7f7f7f7f, 0,
+                                                          0x7f7f7f7f);
+}
+
 // A step is one block of 128 along K: one matrix instruction (16 x 16 x 128) forms
 // the block's sums, which the vector units add with the two scales' product.  The
 // instruction aligns each 8 products to the largest of them and drops what is
@@ -1083,7 +1155,7 @@ struct ProductF8Args {
 template <int TN>
 __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g) {
   constexpr int KS = 128, MI = 4, NI = TN / 32;
-  auto chunk_at = [](int r, int c) { return swizzled<KS / 16>(r, c); };
+  
   __shared__ u32x4 x_lds[kTileRows * KS / 16], w_lds[TN * KS / 16];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
@@ -1130,17 +1202,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
     }
     return v;
   };
-  auto cut = [&](u32x4 a, int k) {
-    const int by = k < at_last ? 0 : k - at_last, bits = 8 * (by % 4);
-    if (at_last < 0) return a;
-    u32x4 o;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = __builtin_amdgcn_alignbit(i < 3 ? a[i + 1] : 0u, a[i], bits);
-    if (by & 4) o = u32x4{o[1], o[2], o[3], 0};
-    if (by & 8) o = u32x4{o[2], o[3], 0, 0};
-    if (by >= 16) o = u32x4{0, 0, 0, 0};
-    return o;
-  };
+  auto cut = [&](u32x4 a, int k) { return at_last < 0 ? a : cut_bytes(a, k < at_last ? 0 : k - at_last); };
   constexpr int NW = TN / 32;
   u32x4 a[4], bw[NW];
   float sx[MI], sw = 0.f;
@@ -1173,31 +1235,28 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
       for (int i = 0; i < NW; ++i) bw[i] = cut(bw[i], k);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x_lds[chunk_at(tid / 8 + 32 * i, tid % 8)] = a[i];
+    for (int i = 0; i < 4; ++i) x_lds[swizzled<8, false>(tid / 8 + 32 * i, tid % 8)] = a[i];
 #pragma unroll
-    for (int i = 0; i < NW; ++i) w_lds[chunk_at(tid / 8 + 32 * i, tid % 8)] = bw[i];
+    for (int i = 0; i < NW; ++i) w_lds[swizzled<8, true>(tid / 8 + 32 * i, tid % 8)] = bw[i];
     lds_sync<4>();
     float sc[MI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) sc[i] = sx[i] * sw;
     if (k0 + KS < K) load(k0 + KS);
     // lane l takes chunks l / 16 and l / 16 + 4 of both operands
-    auto frag = [&](const u32x4 *lds, int r) {
-      const u32x4 lo = lds[chunk_at(r, l / 16)], hi = lds[chunk_at(r, l / 16 + 4)];
-      return i32x8{int(lo[0]), int(lo[1]), int(lo[2]), int(lo[3]), int(hi[0]), int(hi[1]), int(hi[2]), int(hi[3])};
-    };
     i32x8 xf[MI];
 #pragma unroll
-    for (int i = 0; i < MI; ++i) xf[i] = frag(x_lds, wm + 16 * i + l % 16);
+    for (int i = 0; i < MI; ++i) {
+      const int r = wm + 16 * i + l % 16;
+      xf[i] = operand_f8(x_lds[swizzled<8, false>(r, l / 16)], x_lds[swizzled<8, false>(r, l / 16 + 4)]);
+    }
 #pragma unroll
     for (int j = 0; j < NI; ++j) {
-      const i32x8 wf = frag(w_lds, wn + column_of<true>(j, l % 16));
+      const int n = wn + column_of<true>(j, l % 16);
+      const i32x8 wf = operand_f8(w_lds[swizzled<8, true>(n, l / 16)], w_lds[swizzled<8, true>(n, l / 16 + 4)]);
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
-        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        // both block scales of the instruction are 2^(127 - 127)
-        const f32x4 s = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wf, xf[i], zero, 0, 0, 0, 0x7f7f7f7f, 0,
-                                                                         0x7f7f7f7f);
+        const f32x4 s = block_sum_f8(wf, xf[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sc[i], s[e], acc[i][j][e]);
       }
@@ -1216,6 +1275,190 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
       store_row<W>(y + int64_t(mrow[i]) * g.ldy + n, v, N - n);
     }
   }
+}
+
+// The same past weights that stay in LDS (see product_stream_kernel): rows of up to
+// 1152 values for 128 columns.  A wave has 48 rows in flight, its loads a block
+// ahead; a block's sums are scaled as above.
+constexpr int kStreamF8K = kStreamLds / 128;  // longest contraction
+
+__global__ __launch_bounds__(kStreamThreads, 2) void product_f8_stream_kernel(ProductF8Args g) {
+  constexpr int KS = 128, TN = 128, C = KS / 16, MT = 3, NI = TN / 16, RB = 16 * MT;
+  __shared__ u32x4 w_lds[kStreamLds / 16];  // per block of K: TN rows of 128 bytes
+  constexpr int KB = kStreamF8K / KS;
+  __shared__ float ws_lds[KB], xs_lds[kStreamWaves][RB * KB];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
+  const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
+  const int n0 = int(b % g.nt) * TN, K = g.K, N = g.N, kb = (K + KS - 1) / KS, nb = (N + KS - 1) / KS;
+  const int at_last = K - 16;
+  uint16_t *y = g.y;
+  // rows column_of<true>(j, l % 16), chunks l / 16 and l / 16 + 4, of an even and an odd j
+  const int base[2] = {swizzled<C, true>(column_of<true>(0, l % 16), l / 16),
+                       swizzled<C, true>(column_of<true>(1, l % 16), l / 16)};
+  stream_share<RB>(g.offsets, g.rows, g.G, g.M, b / g.nt, g.mt, l, [&](int group, int chunks, auto list) {
+    if (group == g.G) {
+      stream_zeros<RB>(chunks, list, y, g.ldy, n0, n0 + TN < N ? n0 + TN : N, wave, l);
+      return;
+    }
+    auto row_of = [&](int rows, int i) { return __shfl(rows, 16 * i + l % 16); };
+    const uint8_t *w = g.w + int64_t(group) * N * K;
+    int ft = tid;
+    asm volatile("" : "+v"(ft));
+    __syncthreads();  // the group before has been multiplied
+    if (ft < kb) ws_lds[ft] = g.ws[(int64_t(group) * nb + n0 / KS) * kb + ft];
+#pragma unroll 1
+    for (int k0 = 0; k0 < K; k0 += KS) {
+      u32x4 v[2];
+      const int k = k0 + 16 * (ft % 8);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int n = n0 + ft / 8 + 64 * i;  // columns past the last read it, and reach no output
+        v[i] = *reinterpret_cast<const u32x4_any8 *>(w + int64_t(n < N ? n : N - 1) * K + (k < at_last ? k : at_last));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        w_lds[k0 / KS * (TN * C) + swizzled<C, true>(ft / 8 + 64 * i, ft % 8)] = cut_bytes(v[i], k < at_last ? 0 : k - at_last);
+    }
+    __syncthreads();
+    if (wave >= chunks) return;
+    // the loads' side: chunk lc, block lk; next: the rows of the chunk after lc
+    int lc = wave, lk = 0, next = list(lc), lrow[MT];
+    auto point = [&]() {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int r = row_of(next, i);
+        lrow[i] = r < 0 ? 0 : r;
+      }
+      next = list(lc + kStreamWaves);
+    };
+    point();
+    // The rows' scales, kb to a row, pass through LDS: lane i loads those of row i a
+    // chunk ahead.  (Loaded where they are used, 16 rows' lines at a time, they took
+    // as long as a fifth of the kernel.)
+    float *scales = xs_lds[wave];
+    float ahead[KB];
+    auto load_scales = [&](int rows) {
+      const float *p = g.xs + int64_t(rows < 0 ? 0 : rows) * kb;
+#pragma unroll
+      for (int i = 0; i < KB; ++i) ahead[i] = p[i < kb ? i : kb - 1];
+    };
+    auto keep_scales = [&]() {
+      if (l < RB) {
+#pragma unroll
+        for (int i = 0; i < KB; ++i) scales[l * KB + i] = ahead[i];
+      }
+      lds_sync<1>();
+    };
+    struct Rows {
+      u32x4 lo[MT], hi[MT];
+    };
+    auto load = [&](Rows &v) {
+      const int k = lk * KS + 16 * (l / 16), k2 = k + 64;
+      const unsigned at = unsigned(k < at_last ? k : at_last), at2 = unsigned(k2 < at_last ? k2 : at_last);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const uint8_t *p = g.x + int64_t(lrow[i]) * g.ldx;
+        v.lo[i] = *reinterpret_cast<const u32x4_any8 *>(p + at);
+        v.hi[i] = *reinterpret_cast<const u32x4_any8 *>(p + at2);
+      }
+      if (++lk == kb) {
+        lk = 0;
+        lc += kStreamWaves;
+        point();
+      }
+    };
+    f32x4 acc[MT][NI];
+    auto clear = [&]() {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    };
+    clear();
+    int cc = wave, ck = 0, rows = list(cc);  // the products' side
+    auto step = [&](Rows &v) {
+      if (ck * KS + KS > K) {
+        const int k = ck * KS + 16 * (l / 16);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          v.lo[i] = cut_bytes(v.lo[i], k < at_last ? 0 : k - at_last);
+          v.hi[i] = cut_bytes(v.hi[i], k + 64 < at_last ? 0 : k + 64 - at_last);
+        }
+      }
+      i32x8 xf[MT];
+      float sc[MT];
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        xf[i] = operand_f8(v.lo[i], v.hi[i]);
+        sc[i] = scales[(16 * i + l % 16) * KB + ck] * ws_lds[ck];
+      }
+      load(v);
+      const u32x4 *d = w_lds + ck * (TN * C);
+      auto operand = [&](int j) {
+        const u32x4 *p = d + 32 * (j / 2) * C;
+        return operand_f8(p[base[j % 2]], p[base[j % 2] ^ 4]);
+      };
+      // the sums of a product are added under the next one's instructions
+      f32x4 s[MT];
+      i32x8 wf = operand(0);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) s[i] = block_sum_f8(wf, xf[i]);
+      wf = operand(1);
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        f32x4 u[MT];
+        i32x8 wn = wf;
+        if (j + 2 < NI) wn = operand(j + 2);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          if (j + 1 < NI) u[i] = block_sum_f8(wf, xf[i]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][e] = __builtin_fmaf(sc[i], s[i][e], acc[i][j][e]);
+        }
+        wf = wn;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) s[i] = u[i];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+        }
+      }
+      if (++ck < kb) return;
+      int lane = l;
+      asm volatile("" : "+v"(lane));  // keeps the addresses formed here out of the loop's registers
+      // four columns' parts of four rows change lanes, so that a store covers whole
+      // rows of the tile: 256 bytes of four instead of 64 of sixteen
+      const int n = n0 + 32 * (lane % 4) + 8 * (lane / 16);
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        u32x4 v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[q][e] = bf16_pair(acc[i][2 * q + e / 2][2 * (e % 2)], acc[i][2 * q + e / 2][2 * (e % 2) + 1]);
+        quad_transpose(v, lane);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int r = __shfl(rows, 16 * i + (lane % 16 & 12) + q);
+          if (r >= 0) store_bits(y + int64_t(r) * g.ldy + n, v[q], N - n);
+        }
+      }
+      clear();
+      ck = 0;
+      cc += kStreamWaves;
+      rows = list(cc);
+      keep_scales();
+      load_scales(list(cc + kStreamWaves));
+    };
+    Rows v;
+    load(v);
+    load_scales(rows);
+    keep_scales();
+    load_scales(list(cc + kStreamWaves));
+    while (cc < chunks) step(v);
+  });
 }
 
 // ------------------------------------------------------------- launches
@@ -1392,7 +1635,7 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
       (rc = check_rows(X, "X", ldx, K, 1)) || (rc = check_ptr(xs, "xs", 4)) || (rc = check_ptr(W, "W", 1)) ||
       (rc = check_ptr(ws, "ws", 4)) || (rc = check_rows(Y, "Y", ldy, N, 2)))
     return rc;
-  const ProductF8Args g{M,  K,
+  ProductF8Args g{M,  K,
                         N,  G,
                         offsets, rows,
                         static_cast<const uint8_t *>(X), ldx,
@@ -1400,8 +1643,18 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
                         ws, static_cast<uint16_t *>(Y),
                         ldy, int(cdiv(N, N <= 64 ? 64 : 128)),
                         tile_bound(M, G, kTileShift)};
-  const dim3 grid(unsigned(g.mt * g.nt)), block(kThreads);
   hipStream_t s = static_cast<hipStream_t>(stream);
+  // Rows past stationary weights, or tiles, us, 1 and 64 types (before the scales
+  // and stores of the former were gathered): M = 8,000 K = 512 N = 512 13 against 10
+  // and 24 against 14; M = 32,000 24 against 23 and 32 against 29; M = 128,000 56
+  // against 76 and 69 against 83; M = 128,000 K = 128 N = 64 15 against 11.
+  if (N > 64 && K >= 16 && K <= kStreamF8K && M >= 65536 && M >= 1024 * int64_t(G)) {
+    g.nt = int(cdiv(N, 128));
+    g.mt = std::max(1, kStreamGroups / g.nt);
+    hipLaunchKernelGGL(product_f8_stream_kernel, dim3(unsigned(g.mt * g.nt)), dim3(kStreamThreads), 0, s, g);
+    return after("allegro_grouped_matmul_fp8");
+  }
+  const dim3 grid(unsigned(g.mt * g.nt)), block(kThreads);
   if (N <= 64)
     hipLaunchKernelGGL((product_f8_kernel<64>), grid, block, 0, s, g);
   else
