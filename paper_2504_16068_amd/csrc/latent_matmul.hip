@@ -168,11 +168,11 @@ __device__ __forceinline__ u32x4 act_piece(u32x4 v, bool act) {  // of bf16 valu
 // Pieces of the elements k .. of rows of n (k below n or not), row(i) pointing to
 // row i's first one.  The loads are issued without a condition: where a piece
 // crosses the row's end the row's last PE elements are loaded, and shifted down
-// by shift_of when they are used.
-template <class T, int NP, class Row>
+// by shift_of when they are used.  SHORT: rows may have fewer than PE.
+template <class T, bool SHORT, int NP, class Row>
 __device__ __forceinline__ void load_pieces(u32x4 (&v)[NP], Row row, int k, int n) {
   constexpr int PE = Kind<T>::PE;
-  if (n >= PE) {
+  if (!SHORT || n >= PE) {
     const unsigned at = unsigned(k < n - PE ? k : n - PE);
 #pragma unroll
     for (int i = 0; i < NP; ++i) v[i] = *reinterpret_cast<const u32x4_any *>(row(i) + at);
@@ -223,23 +223,24 @@ __device__ __forceinline__ int swizzled(int r, int c) {
 // A tile of `ROWS` rows (of X, or columns of the result) whose contraction runs
 // along memory.  In LDS: rows of KS 16-bit values, in 16-byte chunks swizzled by
 // row so that 8 and 16 lanes reading one chunk of consecutive rows hit distinct
-// banks.  A thread moves pieces tid % 8 of rows tid / 8 + 32 i.
-template <class T, int ROWS, bool WIDE>
+// banks.  NT threads move pieces tid % 8 of rows tid / 8 + RP i.
+template <class T, int ROWS, bool WIDE, int NT = kThreads>
 struct Along {
-  static constexpr int P = Kind<T>::P, KS = Kind<T>::KS, PE = Kind<T>::PE, NP = ROWS / 32, C = KS / 8;
+  static constexpr int P = Kind<T>::P, KS = Kind<T>::KS, PE = Kind<T>::PE, RP = NT / 8, NP = ROWS / RP, C = KS / 8;
   static constexpr int SIZE = P * ROWS * C;  // 16-byte units
   u32x4 v[NP];
-  // row(i): pointer to the first element of row tid / 8 + 32 i; n elements to a row
+  static __device__ __forceinline__ int row(int i, int tid) { return tid / 8 + RP * i; }
+  // row(i): pointer to the first element of row row(i, tid); n elements to a row
   template <class Row>
   __device__ __forceinline__ void load(Row row, int k0, int n, int tid) {
-    load_pieces<T>(v, row, k0 + PE * (tid % 8), n);
+    load_pieces<T, NT == kThreads>(v, row, k0 + PE * (tid % 8), n);
   }
   __device__ __forceinline__ void put(u32x4 *lds, bool act, float scale, int k0, int n, int tid) {
     if (k0 + KS > n) {  // the last step: nothing from n on
 #pragma unroll
       for (int i = 0; i < NP; ++i) v[i] = shifted<T>(v[i], shift_of<T>(k0 + PE * (tid % 8), n));
     }
-    // rows 32 apart are swizzled alike
+    // rows RP apart are swizzled alike
     const int at =
         P == 3 ? 2 * swizzled<C, WIDE>(tid / 8, tid % 8 / 2) + tid % 2 : swizzled<C, WIDE>(tid / 8, tid % 8);
 #pragma unroll
@@ -248,9 +249,9 @@ struct Along {
         u32x2 o[3];
         split_piece(v[i], act, scale, o);
 #pragma unroll
-        for (int p = 0; p < 3; ++p) reinterpret_cast<u32x2 *>(lds)[at + 2 * C * (p * ROWS + 32 * i)] = o[p];
+        for (int p = 0; p < 3; ++p) reinterpret_cast<u32x2 *>(lds)[at + 2 * C * (p * ROWS + RP * i)] = o[p];
       } else {
-        lds[at + C * 32 * i] = act_piece(v[i], act);
+        lds[at + C * RP * i] = act_piece(v[i], act);
       }
     }
   }
@@ -276,28 +277,29 @@ struct Along {
 // LDS load, by which 16 lanes turn 4 rows of 16 columns into 4 rows of one column
 // each.  A wave's load touches 4 columns' quads of 16 rows; chunks (and their
 // halves) are swizzled by row so that those 512 bytes lie in all banks twice.
-template <class T, int COLS, bool WIDE>
+template <class T, int COLS, bool WIDE, int NT = kThreads>
 struct Across {
   static constexpr int P = Kind<T>::P, KS = Kind<T>::KS, PE = Kind<T>::PE;
-  static constexpr int PR = COLS / PE, RP = kThreads / PR, NP = KS / RP;  // pieces to a row, rows to a pass
+  static constexpr int PR = COLS / PE, RP = NT / PR, NP = KS / RP;  // pieces to a row, rows to a pass
   static constexpr int SIZE = P * KS * COLS / 8;                          // 16-byte units
   u32x4 v[NP];
   static __device__ __forceinline__ int quad_at(int k, int c4) {  // in 8-byte units
-    const int f = COLS == 128 ? (k & 3) << 2 | ((k >> 3) & 1) << 1 : ((k >> 1) & 1) << 2 | ((k >> 3) & 1) << 1;
+    const int f = COLS >= 128 ? (k & 3) << 2 | ((k >> 3) & 1) << 1 : ((k >> 1) & 1) << 2 | ((k >> 3) & 1) << 1;
     return k * (COLS / 4) + ((((c4 >> 1) ^ f) << 1) | ((c4 & 1) ^ ((k >> 3) & 1)));
   }
   static __device__ __forceinline__ int step(int i, int tid) { return tid / PR + i * RP; }
   static __device__ __forceinline__ int col(int tid) { return tid % PR * PE; }
-  // row(i): pointer to the first of the tile's columns (n of them exist) of step step(i, tid)
+  // row(i): pointer to the first element of the row of step step(i, tid); the tile's
+  // columns start at c0 of n
   template <class Row>
-  __device__ __forceinline__ void load(Row row, int n, int tid) {
-    load_pieces<T>(v, row, col(tid), n);
+  __device__ __forceinline__ void load(Row row, int c0, int n, int tid) {
+    load_pieces<T, NT == kThreads>(v, row, c0 + col(tid), n);
   }
   // missing: bit i is set if step(i, tid) does not exist and becomes zero
-  __device__ __forceinline__ void put(u32x4 *lds, bool act, float scale, int n, int missing, int tid) {
-    if (n < COLS) {
+  __device__ __forceinline__ void put(u32x4 *lds, bool act, float scale, int c0, int n, int missing, int tid) {
+    if (n - c0 < COLS) {
 #pragma unroll
-      for (int i = 0; i < NP; ++i) v[i] = shifted<T>(v[i], shift_of<T>(col(tid), n));
+      for (int i = 0; i < NP; ++i) v[i] = shifted<T>(v[i], shift_of<T>(c0 + col(tid), n));
     }
     if (__any(missing)) {
 #pragma unroll
@@ -347,12 +349,13 @@ __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) {
 // One contraction step of a wave: MI x NI products of 16 x 16 of the tiles ML (the
 // instructions' columns) and NL (their rows).  fp32 sums are added with the factor
 // `sign`.
-template <class T, class ML, class NL, int MI, int NI>
+template <class T, class ML, class NL, bool TIGHT, int MI, int NI>
 __device__ __forceinline__ void multiply(const u32x4 *m_lds, const u32x4 *n_lds, const typename ML::Reader &m_read,
                                          const typename NL::Reader &n_read, float sign, f32x4 (&acc)[MI][NI]) {
   constexpr int P = Kind<T>::P;
 #pragma unroll
   for (int kk = 0; kk < Kind<T>::KS / 32; ++kk) {
+    if constexpr (TIGHT) __builtin_amdgcn_sched_barrier(0);  // operands of one half at a time
     bf16x8 b[MI][P];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
@@ -512,7 +515,7 @@ __device__ __forceinline__ void list_rows(int *srow, const int32_t *rows, const 
 // Zeros for the rows of a tile, columns n0 .. n0 + n - 1.
 template <class T>
 __device__ __forceinline__ void zero_rows(const int *srow, T *y, int64_t ldy, int n0, int n, int tid) {
-  for (int i = tid; i < kTileRows * n; i += kThreads) {
+  for (int i = tid; i < kTileRows * n; i += int(blockDim.x)) {
     const int r = srow[i / n];
     if (r >= 0) y[int64_t(r) * ldy + n0 + i % n] = T(0);
   }
@@ -536,13 +539,17 @@ struct ProductArgs {
   int64_t mt;  // upper bound of the row tiles
 };
 
+// Threads of a tile TN columns wide: four waves, or eight of a wide one, each with
+// 64 rows and 32 or 64 columns.
+constexpr int tile_threads(int TN) { return TN == 256 ? 2 * kThreads : kThreads; }
+
 template <class T, int TN, bool WT>
-__global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
+__global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void product_kernel(ProductArgs g) {
   constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int MI = 4, NI = TN / 32;
-  using XTile = Along<T, kTileRows, false>;
-  using WTile = std::conditional_t<WT, Along<T, TN, !F32>, Across<T, TN, !F32>>;
+  constexpr int NT = tile_threads(TN), MI = 4, NI = TN / (NT / 128) / 16;
+  using XTile = Along<T, kTileRows, false, NT>;
+  using WTile = std::conditional_t<WT, Along<T, TN, !F32, NT>, Across<T, TN, !F32, NT>>;
   __shared__ u32x4 x_lds[XTile::SIZE], w_lds[WTile::SIZE];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
@@ -558,31 +565,33 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
     return;
   }
   const T *x = static_cast<const T *>(g.x), *w = static_cast<const T *>(g.w) + int64_t(t.g) * K * N;
-  const T *xr[XTile::NP];
+  int xr[XTile::NP];
 #pragma unroll
   for (int i = 0; i < XTile::NP; ++i) {
-    const int r = srow[tid / 8 + 32 * i];
-    xr[i] = x + (r < 0 ? 0 : int64_t(r) * g.ldx);  // rows past the end are multiplied but not stored
+    const int r = srow[XTile::row(i, tid)];
+    xr[i] = r < 0 ? 0 : r;  // rows past the end are multiplied but not stored
   }
   XTile a;
   WTile bw;
   int missing = 0;
   auto load = [&](int k0) {
-    a.load([&](int i) { return xr[i]; }, k0, K, tid);
+    int t = tid;
+    if constexpr (TN == 256) asm volatile("" : "+v"(t));  // addresses are formed anew: 128 registers
+    a.load([&](int i) { return x + int64_t(xr[i]) * g.ldx; }, k0, K, t);
     if constexpr (WT) {
       bw.load(
           [&](int i) {
-            const int n = tid / 8 + 32 * i;  // columns past the last read it, and reach no output
+            const int n = WTile::row(i, t);  // columns past the last read it, and reach no output
             return w + int64_t(n0) * K + (n < N - n0 ? n : N - n0 - 1) * K;
           },
-          k0, K, tid);
+          k0, K, t);
     } else {
       bw.load(
           [&](int i) {
-            const int k = WTile::step(i, tid), left = K - k0;
-            return w + (int64_t(k0) * N + n0) + (k < left ? k : left - 1) * N;
+            const int k = WTile::step(i, t), left = K - k0;
+            return w + int64_t(k0) * N + (k < left ? k : left - 1) * N;
           },
-          N - n0, tid);
+          n0, N, t);
     }
   };
   f32x4 acc[MI][NI];
@@ -590,13 +599,13 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int wm = 64 * (wave % 2), wn = TN / 2 * (wave / 2);
+  const int wm = 64 * (wave % 2), wn = 16 * NI * (wave / 2);
   const typename XTile::Reader x_read(wm / 16, l);
   const typename WTile::Reader w_read(wn / 16, l);
   const float xs = (tid / 8) % 2 ? -kScale : kScale;  // odd rows negated
   load(0);
   for (int k0 = 0; k0 < K; k0 += KS) {
-    lds_sync<4>();  // the previous step has been read
+    lds_sync<NT / kWave>();  // the previous step has been read
     a.put(x_lds, !WT && g.act, xs, k0, K, tid);
     if constexpr (WT) {
       bw.put(w_lds, false, kScale, k0, K, tid);
@@ -605,11 +614,11 @@ __global__ __launch_bounds__(kThreads, 2) void product_kernel(ProductArgs g) {
 #pragma unroll
         for (int i = 0; i < WTile::NP; ++i) missing |= (k0 + WTile::step(i, tid) >= K) << i;
       }
-      bw.put(w_lds, false, kScale, N - n0, missing, tid);
+      bw.put(w_lds, false, kScale, n0, N, missing, tid);
     }
-    lds_sync<4>();
+    lds_sync<NT / kWave>();
     if (k0 + KS < K) load(k0 + KS);
-    multiply<T, XTile, WTile>(x_lds, w_lds, x_read, w_read, 1.f, acc);
+    multiply<T, XTile, WTile, TN == 256>(x_lds, w_lds, x_read, w_read, 1.f, acc);
   }
   if constexpr (F32) {
     if (any_not_finite(acc)) {
@@ -752,9 +761,9 @@ __global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(Produ
         f.load(
             [&](int i) {
               const int k = WTile::step(i, ft), left = K - k0;
-              return w + (int64_t(k0) * N + n0) + (k < left ? k : left - 1) * N;
+              return w + int64_t(k0) * N + (k < left ? k : left - 1) * N;
             },
-            N - n0, ft);
+            n0, N, ft);
       }
     };
     auto fill_put = [&](WTile &f, int tile) {
@@ -765,7 +774,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(Produ
         int missing = 0;
 #pragma unroll
         for (int i = 0; i < WTile::NP; ++i) missing |= (k0 + WTile::step(i, ft) >= K) << i;
-        f.put(w_lds + tile * WTile::SIZE, false, kScale, N - n0, missing, ft);
+        f.put(w_lds + tile * WTile::SIZE, false, kScale, n0, N, missing, ft);
       }
     };
 #pragma unroll 1
@@ -947,12 +956,12 @@ struct WeightArgs {
 // Range k of a group of several goes to slot 2 (offsets[g] >> shift) + k: such a
 // group has more than 1 << shift rows, so the next one's slots start behind it.
 template <class T, int TK, int TN>
-__global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
+__global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void weight_kernel(WeightArgs g) {
   constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int MI = TK / 32, NI = TN / 32;
-  using XTile = Across<T, TK, false>;
-  using YTile = Across<T, TN, false>;
+  constexpr int NT = tile_threads(TN), MI = TK / 32, NI = TN / (NT / 128) / 16;
+  using XTile = Across<T, TK, false, NT>;
+  using YTile = Across<T, TN, false, NT>;
   __shared__ u32x4 x_lds[XTile::SIZE], y_lds[YTile::SIZE];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int tiles = g.kt * g.nt;
@@ -968,53 +977,57 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
   const int k0 = int(b % tiles) / g.nt * TK, n0 = int(b % tiles) % g.nt * TN, K = g.K, N = g.N;
   const T *x = static_cast<const T *>(g.x), *dy = static_cast<const T *>(g.dy);
   auto row_of = [&](int64_t i) -> int {
-    if (i >= end) return -1;
-    const int64_t r = g.rows ? int64_t(g.rows[i]) : i;
-    return r < 0 || r >= g.M ? -1 : int(r);
+    const int64_t in = i < end ? i : end - 1;
+    const int r = g.rows ? g.rows[in] : int(in);
+    return i < end && r >= 0 && r < g.M ? r : -1;
   };
   XTile xa;
   YTile ya;
-  // list entries of the next step, loaded a step ahead; bit i of missing: none
-  int xr[XTile::NP], yr[YTile::NP], xm = 0, ym = 0;
-  auto list = [&](int64_t m) {
-#pragma unroll
-    for (int i = 0; i < XTile::NP; ++i) xr[i] = row_of(m + XTile::step(i, tid));
-#pragma unroll
-    for (int i = 0; i < YTile::NP; ++i) yr[i] = TK == TN ? xr[i < XTile::NP ? i : 0] : row_of(m + YTile::step(i, tid));
-  };
+  // rows: lane i has the list's entry i of the next step, loaded a step ahead; bit i
+  // of xm and ym: the step at hand has no row step(i, tid)
+  int rows = 0, xm = 0, ym = 0;
   auto load = [&]() {
+    int t = tid;
+    if constexpr (TN == 256) asm volatile("" : "+v"(t));  // addresses are formed anew: 128 registers
+    int xr[XTile::NP], yr[YTile::NP];
     xm = ym = 0;
 #pragma unroll
-    for (int i = 0; i < XTile::NP; ++i) xm |= int(xr[i] < 0) << i;
+    for (int i = 0; i < XTile::NP; ++i) {
+      xr[i] = __shfl(rows, XTile::step(i, t));
+      xm |= int(xr[i] < 0) << i;
+    }
 #pragma unroll
-    for (int i = 0; i < YTile::NP; ++i) ym |= int(yr[i] < 0) << i;
-    xa.load([&](int i) { return x + k0 + (xr[i] < 0 ? 0 : int64_t(xr[i]) * g.ldx); }, K - k0, tid);
-    ya.load([&](int i) { return dy + n0 + (yr[i] < 0 ? 0 : int64_t(yr[i]) * g.lddy); }, N - n0, tid);
+    for (int i = 0; i < YTile::NP; ++i) {
+      yr[i] = __shfl(rows, YTile::step(i, t));
+      ym |= int(yr[i] < 0) << i;
+    }
+    xa.load([&](int i) { return x + (xr[i] < 0 ? 0 : int64_t(xr[i]) * g.ldx); }, k0, K, t);
+    ya.load([&](int i) { return dy + (yr[i] < 0 ? 0 : int64_t(yr[i]) * g.lddy); }, n0, N, t);
   };
   f32x4 acc[MI][NI];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int wk = TK / 2 * (wave % 2), wn = TN / 2 * (wave / 2);
+  const int wk = TK / 2 * (wave % 2), wn = 16 * NI * (wave / 2);
   const typename XTile::Reader x_read(wk / 16, l);
   const typename YTile::Reader y_read(wn / 16, l);
   float sign = 1.f;
   if (t.m0 < end) {
-    list(t.m0);
+    rows = row_of(t.m0 + l % KS);
     load();
-    list(t.m0 + KS);
+    rows = row_of(t.m0 + KS + l % KS);
   }
   for (int64_t m = t.m0; m < end; m += KS) {
-    lds_sync<4>();
-    xa.put(x_lds, g.act, sign * kScale, K - k0, xm, tid);
-    ya.put(y_lds, false, kScale, N - n0, ym, tid);
-    lds_sync<4>();
+    lds_sync<NT / kWave>();
+    xa.put(x_lds, g.act, sign * kScale, k0, K, xm, tid);
+    ya.put(y_lds, false, kScale, n0, N, ym, tid);
+    lds_sync<NT / kWave>();
     if (m + KS < end) {
       load();
-      list(m + 2 * KS);
+      rows = row_of(m + 2 * KS + l % KS);
     }
-    multiply<T, XTile, YTile>(x_lds, y_lds, x_read, y_read, sign, acc);
+    multiply<T, XTile, YTile, TN == 256>(x_lds, y_lds, x_read, y_read, sign, acc);
     sign = -sign;
   }
   if constexpr (F32) {
@@ -1022,15 +1035,15 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
       multiply_again(
           acc, end - t.m0, l,
           [&](int i, int64_t m) {
-            const int64_t r = row_of(t.m0 + m);
+            const int r = row_of(t.m0 + m);
             const int k = k0 + wk + 16 * i + l % 16;
-            const float v = r < 0 || k >= K ? 0.f : x[r * g.ldx + k];
+            const float v = r < 0 || k >= K ? 0.f : x[int64_t(r) * g.ldx + k];
             return g.act ? silu(v) : v;
           },
           [&](int j, int64_t m) {
-            const int64_t r = row_of(t.m0 + m);
+            const int r = row_of(t.m0 + m);
             const int n = n0 + wn + 16 * j + l % 16;
-            return r < 0 || n >= N ? 0.f : dy[r * g.lddy + n];
+            return r < 0 || n >= N ? 0.f : dy[int64_t(r) * g.lddy + n];
           });
     } else {
 #pragma unroll
@@ -1058,11 +1071,14 @@ __global__ __launch_bounds__(kThreads, 2) void weight_kernel(WeightArgs g) {
   }
 }
 
-// Workgroup (e, y): elements 256 e .. of the y-th group that has several ranges.
-constexpr int kSumThreads = 512;
-template <class T>
+// Workgroup (e, y): elements of the y-th group that has several ranges.  SPLIT: 256
+// elements, whose ranges the waves share; else 256 for every wave, which adds all
+// ranges: where there are that many elements (1024 x 512 of 24 ranges: 54 us
+// with SPLIT).
+constexpr int kSumThreads = 512, kSumWaves = kSumThreads / kWave;
+template <class T, bool SPLIT>
 __global__ __launch_bounds__(kSumThreads) void weight_sum_kernel(WeightArgs g) {
-  __shared__ f32x4 sums[kSumThreads / kWave][kWave];
+  __shared__ f32x4 sums[SPLIT ? kSumWaves : 1][kWave];
   const int tid = threadIdx.x, l = tid % kWave, wave = tid / kWave;
   auto clamped = [&](int i) {
     const int64_t o = g.offsets[i];
@@ -1084,18 +1100,22 @@ __global__ __launch_bounds__(kSumThreads) void weight_sum_kernel(WeightArgs g) {
   if (found < 0) return;
   const int64_t begin = clamped(found), rows = clamped(found + 1) - begin, KN = int64_t(g.K) * g.N;
   const int ranges = int((rows + (int64_t(1) << g.shift) - 1) >> g.shift);
-  const int64_t e = int64_t(blockIdx.x) * 256 + 4 * l;
+  const int64_t e = (SPLIT ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * kSumWaves + wave) * 256 + 4 * l;
+  const int first = SPLIT ? wave : 0, step = SPLIT ? kSumWaves : 1;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (e < KN) {
     const float *p = g.part + 2 * (begin >> g.shift) * g.slot + e;  // slots are padded to whole vectors
-#pragma unroll 4
-    for (int k = wave; k < ranges; k += kSumThreads / kWave) s += *reinterpret_cast<const f32x4 *>(p + k * g.slot);
+#pragma unroll 8
+    for (int k = first; k < ranges; k += step) s += *reinterpret_cast<const f32x4 *>(p + k * g.slot);
   }
-  sums[wave][l] = s;
-  __syncthreads();
-  if (wave || e >= KN) return;
+  if constexpr (SPLIT) {
+    sums[wave][l] = s;
+    __syncthreads();
+    if (wave) return;
 #pragma unroll
-  for (int k = 1; k < kSumThreads / kWave; ++k) s += sums[k][l];
+    for (int k = 1; k < kSumWaves; ++k) s += sums[k][l];
+  }
+  if (e >= KN) return;
   T *o = static_cast<T *>(g.dw) + int64_t(found) * KN + e;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -1484,6 +1504,18 @@ void launch_product(ProductArgs g, hipStream_t s) {
     }
   }
   g.mt = tile_bound(g.M, g.G, kTileShift);
+  if constexpr (sizeof(T) == 2 && !WT) {
+    // 256 columns at a time, so that a row's SiLU is computed half as often: K = 512,
+    // N = 512, us, 1 and 100 types: M = 32,000 38 against 29 and 50 against 46,
+    // M = 400,000 394 against 352 and 415 against 358; K = 1024 and one type 68
+    // against 49; M = 2,000 16 against 19.  Without SiLU and for the gradient of X
+    // both are within 5%.
+    if (g.act && g.N > 128 && g.K >= 256 && g.M >= 16384) {
+      g.nt = int(cdiv(g.N, 256));
+      hipLaunchKernelGGL((product_kernel<T, 256, false>), dim3(unsigned(g.mt * g.nt)), dim3(tile_threads(256)), 0, s, g);
+      return;
+    }
+  }
   const dim3 grid(unsigned(g.mt * g.nt)), block(kThreads);
   if (narrow)
     hipLaunchKernelGGL((product_kernel<T, 64, WT>), grid, block, 0, s, g);
@@ -1515,8 +1547,18 @@ void launch_weight(WeightArgs g, const WeightShape &z, hipStream_t s) {
   g.nt = z.nt;
   g.slot = z.slot;
   g.ranges = tile_bound(g.M, g.G, z.shift);
+  const bool wide = sizeof(T) == 2 && g.K > 64 && g.N > 128 && g.M * g.kt * g.nt >= 131072;
+  if (wide) g.nt = int(cdiv(g.N, 256));
   const dim3 grid(unsigned(g.ranges * g.kt * g.nt)), block(kThreads);
-  if (g.K <= 64 && g.N <= 64)
+  if constexpr (sizeof(T) == 2) {
+    // 256 columns of dW at a time, us, 1 and 100 types: K = 128, N = 256 M = 32,000 23
+    // against 25, 100,000 44 against 38 and 60 against 54; K = 512, N = 512 M = 2,000 20
+    // against 23, 32,000 66 against 57, 400,000 584 against 445 and 497 against 484
+    if (wide) hipLaunchKernelGGL((weight_kernel<T, 128, 256>), grid, dim3(tile_threads(256)), 0, s, g);
+  }
+  if (wide)
+    ;
+  else if (g.K <= 64 && g.N <= 64)
     hipLaunchKernelGGL((weight_kernel<T, 64, 64>), grid, block, 0, s, g);
   else if (g.K <= 64)
     hipLaunchKernelGGL((weight_kernel<T, 64, 128>), grid, block, 0, s, g);
@@ -1526,8 +1568,12 @@ void launch_weight(WeightArgs g, const WeightShape &z, hipStream_t s) {
     hipLaunchKernelGGL((weight_kernel<T, 128, 128>), grid, block, 0, s, g);
   if (z.slots) {
     const unsigned several = unsigned(std::min<int64_t>(g.G, g.M >> z.shift));
-    hipLaunchKernelGGL((weight_sum_kernel<T>), dim3(unsigned(cdiv(int64_t(g.K) * g.N, 256)), several),
-                       dim3(kSumThreads), 0, s, g);
+    const int64_t parts = cdiv(int64_t(g.K) * g.N, 256);
+    if (parts * several < 4096)
+      hipLaunchKernelGGL((weight_sum_kernel<T, true>), dim3(unsigned(parts), several), dim3(kSumThreads), 0, s, g);
+    else
+      hipLaunchKernelGGL((weight_sum_kernel<T, false>), dim3(unsigned(cdiv(parts, kSumWaves)), several),
+                         dim3(kSumThreads), 0, s, g);
   }
 }
 

@@ -38,7 +38,7 @@ constexpr int kOneChunk = 4096;  // rows that one workgroup takes alone
 
 __host__ __device__ inline int64_t chunk_rows(int64_t M) {  // at most 1024 chunks
   const int64_t c = (M + 1023) / 1024;
-  return c <= 2048 ? 2048 : (c + 1023) / 1024 * 1024;
+  return c <= 2048 ? 2048 : (c + 2047) / 2048 * 2048;
 }
 
 __device__ __forceinline__ int key_of(const int32_t *type, int64_t r, int G) {
@@ -145,7 +145,7 @@ __global__ __launch_bounds__(kThreads) void group_one_kernel(int M, int G, int b
   place_rows(type, lo, hi, G, bits, count[wave], rows, M, lane);
 }
 
-__global__ __launch_bounds__(kThreads) void group_count_kernel(int64_t M, int G, int64_t chunk, int chunks,
+__global__ __launch_bounds__(kThreads) void group_count_kernel(int64_t M, int G, int64_t chunk,
                                                                const int32_t *__restrict__ type,
                                                                int *__restrict__ hist) {
   __shared__ int count[kMaxGroups + 1];
@@ -155,69 +155,106 @@ __global__ __launch_bounds__(kThreads) void group_count_kernel(int64_t M, int G,
   const int64_t lo = chunk * blockIdx.x, hi = lo + chunk < M ? lo + chunk : M;
   for (int64_t r = lo + tid; r < hi; r += kThreads) atomicAdd(&count[key_of(type, r, G)], 1);
   __syncthreads();
-  for (int i = tid; i <= G; i += kThreads) hist[int64_t(i) * chunks + blockIdx.x] = count[i];
+  for (int i = tid; i <= G; i += kThreads) hist[int64_t(blockIdx.x) * (G + 1) + i] = count[i];
 }
 
-// Workgroup g: hist[g][.] becomes its exclusive sums over the (at most 1024)
-// chunks, total[g] the whole.
-__global__ __launch_bounds__(kThreads) void group_scan_kernel(int chunks, int *__restrict__ hist,
-                                                              int *__restrict__ total) {
-  __shared__ int tmp[kWaves];
-  const int tid = threadIdx.x;
-  int *h = hist + int64_t(blockIdx.x) * chunks;
-  constexpr int PER = 1024 / kThreads;
-  int v[PER], sum = 0, all;
+// A workgroup has 16 types; its 64 threads for each share the (at most 1024)
+// chunks.  hist[.][g] becomes its exclusive sums over the chunks, total[g] the whole.
+constexpr int kScanTypes = 16, kScanParts = 64;
+__global__ __launch_bounds__(kScanTypes *kScanParts) void group_scan_kernel(int chunks, int G, int *__restrict__ hist,
+                                                                          int *__restrict__ total) {
+  __shared__ int sums[kScanParts][kScanTypes];
+  const int i = threadIdx.x % kScanTypes, part = threadIdx.x / kScanTypes, g = blockIdx.x * kScanTypes + i;
+  constexpr int PER = 1024 / kScanParts;
+  const int per = (chunks + kScanParts - 1) / kScanParts, lo = part * per;
+  const int n = g > G || lo >= chunks ? 0 : lo + per < chunks ? per : chunks - lo;
+  int v[PER], sum = 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    v[i] = PER * tid + i < chunks ? h[PER * tid + i] : 0;
-    sum += v[i];
-  }
-  int at = block_exclusive(sum, tmp, all, tid);
+  for (int c = 0; c < PER; ++c) v[c] = c < n ? hist[int64_t(lo + c) * (G + 1) + g] : 0;
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    if (PER * tid + i < chunks) h[PER * tid + i] = at;
-    at += v[i];
+  for (int c = 0; c < PER; ++c) sum += v[c];
+  sums[part][i] = sum;
+  __syncthreads();
+  int at = 0;
+#pragma unroll 8
+  for (int p = 0; p < part; ++p) at += sums[p][i];
+#pragma unroll
+  for (int c = 0; c < PER; ++c) {
+    if (c < n) hist[int64_t(lo + c) * (G + 1) + g] = at;
+    at += v[c];
   }
-  if (tid == 0) total[blockIdx.x] = all;
+  if (part == kScanParts - 1 && g <= G) total[g] = at;
 }
 
-__global__ __launch_bounds__(kThreads) void group_place_kernel(int64_t M, int G, int bits, int64_t chunk, int chunks,
+// A chunk goes through in parts of kPart rows, each wave with consecutive rows: a
+// row's rank among its wave's rows of its type, then the places of each wave's
+// first row of each type, then the rows to their places.
+constexpr int kPart = 2048, kPartSteps = kPart / kThreads;
+__global__ __launch_bounds__(kThreads) void group_place_kernel(int64_t M, int G, int bits, int64_t chunk,
                                                                const int32_t *__restrict__ type,
                                                                const int *__restrict__ hist,
                                                                const int *__restrict__ total,
                                                                int64_t *__restrict__ offsets,
                                                                int32_t *__restrict__ rows) {
-  __shared__ int count[kWaves][kMaxGroups + 1];
+  __shared__ int count[kWaves][kMaxGroups + 1], first[kMaxGroups + 1];
   __shared__ int tmp[kWaves];
   const int tid = threadIdx.x, wave = tid / kWave, lane = tid % kWave;
-  for (int w = 0; w < kWaves; ++w)
-    for (int i = tid; i <= G; i += kThreads) count[w][i] = 0;
-  __syncthreads();
-  const int64_t c0 = chunk * blockIdx.x, n = c0 + chunk < M ? chunk : M - c0;
-  int64_t lo, hi;
-  part_of(n, wave, lo, hi);
-  lo += c0;
-  hi += c0;
-  count_rows(type, lo, hi, G, count[wave], lane);
-  __syncthreads();
-  int base = 0;
+  const int64_t c0 = chunk * blockIdx.x, c1 = c0 + chunk < M ? c0 + chunk : M;
+  int key[kPartSteps], rank[kPartSteps];
+  auto load_keys = [&](int64_t part) {
+    const int64_t r0 = part + wave * (kPart / kWaves) + lane;
+#pragma unroll
+    for (int s = 0; s < kPartSteps; ++s) key[s] = r0 + s * kWave < c1 ? key_of(type, r0 + s * kWave, G) : -1;
+  };
+  load_keys(c0);
+  int sum = 0;
   for (int g0 = 0; g0 <= G; g0 += kThreads) {
     const int g = g0 + tid;
+    const int here = g <= G ? hist[int64_t(blockIdx.x) * (G + 1) + g] : 0;
     int all;
-    const int first = base + block_exclusive(g <= G ? total[g] : 0, tmp, all, tid);
+    const int at = sum + block_exclusive(g <= G ? total[g] : 0, tmp, all, tid);
     if (g <= G) {
-      if (blockIdx.x == 0) offsets[g] = first;
-      int at = first + hist[int64_t(g) * chunks + blockIdx.x];
-      for (int w = 0; w < kWaves; ++w) {
-        const int c = count[w][g];
-        count[w][g] = at;
-        at += c;
-      }
+      if (blockIdx.x == 0) offsets[g] = at;
+      first[g] = at + here;
     }
-    base += all;
+    sum += all;
   }
-  __syncthreads();
-  place_rows(type, lo, hi, G, bits, count[wave], rows, M, lane);
+  for (int64_t part = c0; part < c1; part += kPart) {
+    for (int w = 0; w < kWaves; ++w)
+      for (int i = tid; i <= G; i += kThreads) count[w][i] = 0;
+    __syncthreads();
+    const int64_t r0 = part + wave * (kPart / kWaves) + lane;
+    uint64_t peers[kPartSteps];
+#pragma unroll
+    for (int s = 0; s < kPartSteps; ++s) peers[s] = same_key(key[s], bits, __ballot(key[s] >= 0));
+#pragma unroll
+    for (int s = 0; s < kPartSteps; ++s) {
+      const bool on = key[s] >= 0;
+      const int before = __popcll(peers[s] & ((uint64_t(1) << lane) - 1));
+      const int base = on ? count[wave][key[s]] : 0;
+      allegro_dev::lds_sync<1>();  // every lane has read its counter
+      if (on && before == 0) count[wave][key[s]] = base + __popcll(peers[s]);
+      allegro_dev::lds_sync<1>();
+      rank[s] = base + before;
+    }
+    __syncthreads();
+    for (int g = tid; g <= G; g += kThreads) {
+      int at = first[g];
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const int n = count[w][g];
+        count[w][g] = at;
+        at += n;
+      }
+      first[g] = at;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < kPartSteps; ++s)
+      if (key[s] >= 0) rows[count[wave][key[s]] + rank[s]] = int32_t(r0 + s * kWave);
+    if (part + kPart < c1) load_keys(part + kPart);
+    __syncthreads();
+  }
 }
 
 __global__ void zero_kernel(int64_t n, float *p) {
@@ -860,10 +897,11 @@ int allegro_group_rows(int64_t M, int G, const int32_t *type, int64_t *offsets, 
   const int64_t chunk = chunk_rows(M);
   const int chunks = int(cdiv(M, chunk));
   int *hist = static_cast<int *>(workspace), *total = hist + int64_t(G + 1) * chunks;
-  hipLaunchKernelGGL(group_count_kernel, dim3(chunks), dim3(kThreads), 0, s, M, G, chunk, chunks, type, hist);
-  hipLaunchKernelGGL(group_scan_kernel, dim3(G + 1), dim3(kThreads), 0, s, chunks, hist, total);
-  hipLaunchKernelGGL(group_place_kernel, dim3(chunks), dim3(kThreads), 0, s, M, G, bits, chunk, chunks, type, hist,
-                     total, offsets, rows);
+  hipLaunchKernelGGL(group_count_kernel, dim3(chunks), dim3(kThreads), 0, s, M, G, chunk, type, hist);
+  hipLaunchKernelGGL(group_scan_kernel, dim3(unsigned(cdiv(G + 1, kScanTypes))),
+                     dim3(kScanTypes * kScanParts), 0, s, chunks, G, hist, total);
+  hipLaunchKernelGGL(group_place_kernel, dim3(chunks), dim3(kThreads), 0, s, M, G, bits, chunk, type, hist, total,
+                     offsets, rows);
   return after("allegro_group_rows");
 }
 
