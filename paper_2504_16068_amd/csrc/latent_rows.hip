@@ -821,11 +821,14 @@ void norm_backward(NormBackArgs g, float *dw, hipStream_t s) {
   int64_t grid = 0;
   if (!with_shape<T>(g.C, z.nv, [&](auto vw, auto nv) {
         grid = std::min<int64_t>(cdiv(g.M, kThreads / z.lanes * norm_rows<vw(), nv(), 8>()), kBackGroups);
+        if (grid == 1) g.part = dw;  // few rows: no sums over workgroups
         hipLaunchKernelGGL((norm_backward_kernel<T, vw(), nv()>), dim3(unsigned(grid)), dim3(kThreads), 0, s, g);
       })) {
     grid = back_groups(g.M);
+    if (grid == 1) g.part = dw;
     hipLaunchKernelGGL((norm_wide_backward_kernel<T>), dim3(unsigned(grid)), dim3(kThreads), 0, s, g);
   }
+  if (grid == 1) return;
   hipLaunchKernelGGL(column_sum_kernel, dim3(unsigned(cdiv(g.C, kSumCols))), dim3(kSumCols * kSumGroups), 0, s,
                      int(grid), g.C, g.part, dw);
 }

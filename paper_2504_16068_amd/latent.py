@@ -15,7 +15,7 @@ import os
 
 import torch
 
-from .binding import ALLEGRO_OK, AllegroError, _need, _ptr, _stream
+from .binding import ALLEGRO_OK, AllegroError, _raw_stream
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liballegro_latent.so")
@@ -75,91 +75,128 @@ def _check(rc: int):
         raise AllegroError(rc, allegro_latent_last_error())
 
 
-_DTYPES = {torch.float32: ALLEGRO_F32, torch.bfloat16: ALLEGRO_BF16}
+_Tensor = torch.Tensor
+_F32, _BF16, _F8, _I32, _I64 = torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.int32, torch.int64
+
+# As in binding.py, an argument that is right takes one pass of cheap comparisons
+# (device indices instead of device objects, contiguity before strides): a call with
+# six tensors costs 5 us before its launch that way, 6 with objects and strides.
 
 
-def _dtype(t, name):
-    code = _DTYPES.get(t.dtype) if isinstance(t, torch.Tensor) else None
-    if code is None:
-        raise TypeError(f"{name} must be a float32 or bfloat16 torch.Tensor")
-    return code
-
-
-def _rows(t, name, shape, dtype, device):
-    """Checks a tensor of rows and returns its row stride in elements."""
-    if not isinstance(t, torch.Tensor):
+def _matrix(t, name):
+    """(dtype code, device index) of a float32 or bfloat16 matrix on a GPU."""
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a torch.Tensor")
-    if t.device != device or not t.is_cuda:
-        raise ValueError(f"{name} must live on {device}, a GPU")
+    dt = t.dtype
+    if dt is not _F32 and dt is not _BF16:
+        raise TypeError(f"{name} must be float32 or bfloat16, got {dt}")
+    return 0 if dt is _F32 else 1, _index(t, name)
+
+
+def _index(t, name):
+    if t.dim() != 2:
+        raise ValueError(f"{name} must have two dimensions, got shape {tuple(t.shape)}")
+    index = t.get_device()
+    if index < 0:
+        raise ValueError(f"{name} must live on a GPU, not on {t.device}")
+    return index
+
+
+def _refuse(t, name, shape, dtype, index):
+    if not isinstance(t, _Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor")
+    if t.get_device() != index:
+        raise ValueError(f"{name} must live on cuda:{index}, not on {t.device}")
     if t.dtype is not dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)}")
-    m, c = shape
-    if m == 0 or c == 0:
-        return c
+
+
+def _rows(t, name, shape, dtype, index):
+    """Checks a tensor of rows and returns its row stride in elements."""
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index):
+        _refuse(t, name, shape, dtype, index)
+    if t.is_contiguous():
+        return shape[1]
     s0, s1 = t.stride()
+    m, c = shape
     if (s1 != 1 and c > 1) or (s0 < c and m > 1):
         raise ValueError(f"{name} must have unit column stride and rows that do not overlap, got strides {(s0, s1)}")
-    return s0 if m > 1 else max(s0, c)
+    return s0 if m > 1 else c
 
 
-def _matrix(t, name):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor")
-    if t.dim() != 2:
-        raise ValueError(f"{name} must have two dimensions, got shape {tuple(t.shape)}")
-    return t.shape
+def _whole(t, name, shape, dtype, index):
+    """Checks a contiguous tensor and returns its address."""
+    if not (isinstance(t, _Tensor) and t.dtype is dtype and t.shape == shape and t.get_device() == index):
+        _refuse(t, name, shape, dtype, index)
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
 
 
-def _groups(w, dims, offsets, rows, M, dev):
-    """Checks weights [G, ., .] and the grouping of M rows; returns w's shape."""
-    if not isinstance(w, torch.Tensor):
+def _weights(w, dims):
+    if not isinstance(w, _Tensor):
         raise TypeError("w must be a torch.Tensor")
     if w.dim() != 3:
         raise ValueError(f"w must be [G, {dims}], got shape {tuple(w.shape)}")
-    if offsets is not None:
-        _need(offsets, "offsets", (w.shape[0] + 1,), torch.int64, dev)
-    if rows is not None:
-        _need(rows, "rows", (M,), torch.int32, dev)
     return w.shape
 
 
-def _scratch(t, need, device):
+def _groups(offsets, rows, g, m, index):
+    """Addresses of the grouping of m rows."""
+    return (0 if offsets is None else _whole(offsets, "offsets", (g + 1,), _I64, index),
+            0 if rows is None else _whole(rows, "rows", (m,), _I32, index))
+
+
+def _scratch(t, need, index):
+    """(tensor that keeps it, address, bytes) of a workspace."""
     if need == 0:
-        return 0, 0
+        return None, 0, 0
     if t is None:
-        t = torch.empty(need, dtype=torch.uint8, device=device)
-    elif not isinstance(t, torch.Tensor) or t.device != device or not t.is_contiguous():
-        raise ValueError(f"workspace must be a contiguous tensor on {device}")
-    return t.data_ptr(), t.numel() * t.element_size()
+        t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
+        return t, t.data_ptr(), need
+    if not isinstance(t, _Tensor) or t.get_device() != index or not t.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
+    return t, t.data_ptr(), t.numel() * t.element_size()
+
+
+def _stream_of(stream, index):
+    if stream is None:
+        return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
+    return stream.cuda_stream
+
+
+def _bytes(fn, *sizes):
+    out = ctypes.c_size_t()
+    _check(fn(*(int(v) for v in sizes), ctypes.byref(out)))
+    return out.value
 
 
 # ---------------------------------------------------------------- grouping
 
 def allegro_group_rows_workspace(n_rows: int, n_groups: int) -> int:
     """Bytes of workspace allegro_group_rows needs."""
-    out = ctypes.c_size_t()
-    _check(_lib.allegro_group_rows_workspace(int(n_rows), int(n_groups), ctypes.byref(out)))
-    return out.value
+    return _bytes(_lib.allegro_group_rows_workspace, n_rows, n_groups)
 
 
 def allegro_group_rows(types, n_groups: int, offsets=None, rows=None, workspace=None, stream=None):
     """Returns (offsets [G+1] int64, rows [M] int32): the rows of each type 0 .. G-1 in order, from types [M]
     int32; rows of any other type come last."""
-    if not isinstance(types, torch.Tensor):
+    if not isinstance(types, _Tensor):
         raise TypeError("types must be a torch.Tensor")
-    dev, m, g = types.device, types.numel(), int(n_groups)
-    _need(types, "types", (m,), torch.int32, dev)
+    m, g, index = types.numel(), int(n_groups), types.get_device()
+    if index < 0:
+        raise ValueError(f"types must live on a GPU, not on {types.device}")
     need = allegro_group_rows_workspace(m, g)
     if offsets is None:
-        offsets = torch.empty(g + 1, dtype=torch.int64, device=dev)
+        offsets = torch.empty(g + 1, dtype=_I64, device=types.device)
     if rows is None:
-        rows = torch.empty(m, dtype=torch.int32, device=dev)
-    _need(offsets, "offsets", (g + 1,), torch.int64, dev)
-    _need(rows, "rows", (m,), torch.int32, dev)
-    ws, ws_bytes = _scratch(workspace, need, dev)
-    _check(_lib.allegro_group_rows(m, g, _ptr(types), _ptr(offsets), _ptr(rows), ws, ws_bytes, _stream(stream, dev)))
+        rows = torch.empty(m, dtype=_I32, device=types.device)
+    t_p = _whole(types, "types", (m,), _I32, index)
+    o_p, r_p = _groups(offsets, rows, g, m, index)
+    keep, ws, ws_bytes = _scratch(workspace, need, index)
+    _check(_lib.allegro_group_rows(m, g, t_p, o_p, r_p, ws, ws_bytes, _stream_of(stream, index)))
     return offsets, rows
 
 
@@ -167,143 +204,141 @@ def allegro_group_rows(types, n_groups: int, offsets=None, rows=None, workspace=
 
 def allegro_grouped_matmul(x, w, offsets, rows=None, act: int = ALLEGRO_ACT_NONE, out=None, stream=None):
     """Returns y [M, N]: act(x[r]) @ w[type of r] for x [M, K] and w [G, K, N]; zeros for rows without a type."""
-    code = _dtype(x, "x")
-    m, k = _matrix(x, "x")
-    dev = x.device
-    g, wk, n = _groups(w, "K, N", offsets, rows, m, dev)
-    _need(w, "w", (g, k, n), x.dtype, dev)
+    g, _, n = _weights(w, "K, N")
+    code, index = _matrix(x, "x")
+    dt, shape = x.dtype, x.shape
+    m, k = shape
     if out is None:
-        out = torch.empty((m, n), dtype=x.dtype, device=dev)
-    ldx, ldy = _rows(x, "x", (m, k), x.dtype, dev), _rows(out, "out", (m, n), x.dtype, dev)
-    _check(_lib.allegro_grouped_matmul(code, int(act), m, k, n, g, _ptr(offsets), _ptr(rows), _ptr(x), ldx, _ptr(w),
-                                       _ptr(out), ldy, _stream(stream, dev)))
+        out = torch.empty((m, n), dtype=dt, device=x.device)
+    w_p = _whole(w, "w", (g, k, n), dt, index)
+    o_p, r_p = _groups(offsets, rows, g, m, index)
+    ldx, ldy = _rows(x, "x", shape, dt, index), _rows(out, "out", (m, n), dt, index)
+    _check(_lib.allegro_grouped_matmul(code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, w_p, out.data_ptr(), ldy,
+                                       _stream_of(stream, index)))
     return out
 
 
 def allegro_grouped_matmul_workspace(n_rows: int, k: int, n: int, n_groups: int) -> int:
     """Bytes of workspace allegro_grouped_matmul_backward needs for dw."""
-    out = ctypes.c_size_t()
-    _check(_lib.allegro_grouped_matmul_workspace(int(n_rows), int(k), int(n), int(n_groups), ctypes.byref(out)))
-    return out.value
+    return _bytes(_lib.allegro_grouped_matmul_workspace, n_rows, k, n, n_groups)
 
 
 def allegro_grouped_matmul_backward(x, w, dy, offsets, rows=None, act: int = ALLEGRO_ACT_NONE, dx=None, dw=None,
                                     need_dx: bool = True, need_dw: bool = True, workspace=None, stream=None):
     """Returns (dx [M, K], dw [G, K, N]) of allegro_grouped_matmul; None for one that is not needed."""
-    code = _dtype(x, "x")
-    m, k = _matrix(x, "x")
-    dev = x.device
-    g, wk, n = _groups(w, "K, N", offsets, rows, m, dev)
-    _need(w, "w", (g, k, n), x.dtype, dev)
-    ldx, lddy, lddx = _rows(x, "x", (m, k), x.dtype, dev), _rows(dy, "dy", (m, n), x.dtype, dev), k
-    ws = ws_bytes = 0
+    g, _, n = _weights(w, "K, N")
+    code, index = _matrix(x, "x")
+    dt, shape = x.dtype, x.shape
+    m, k = shape
+    w_p = _whole(w, "w", (g, k, n), dt, index)
+    o_p, r_p = _groups(offsets, rows, g, m, index)
+    ldx, lddy = _rows(x, "x", shape, dt, index), _rows(dy, "dy", (m, n), dt, index)
+    dx_p, lddx, dw_p, keep, ws, ws_bytes = 0, k, 0, None, 0, 0
     if need_dx:
         if dx is None:
-            dx = torch.empty((m, k), dtype=x.dtype, device=dev)
-        lddx = _rows(dx, "dx", (m, k), x.dtype, dev)
+            dx = torch.empty((m, k), dtype=dt, device=x.device)
+        dx_p, lddx = dx.data_ptr(), _rows(dx, "dx", shape, dt, index)
     if need_dw:
         if dw is None:
-            dw = torch.empty((g, k, n), dtype=x.dtype, device=dev)
-        _need(dw, "dw", (g, k, n), x.dtype, dev)
-        ws, ws_bytes = _scratch(workspace, allegro_grouped_matmul_workspace(m, k, n, g), dev)
-    dx, dw = dx if need_dx else None, dw if need_dw else None
-    _check(_lib.allegro_grouped_matmul_backward(code, int(act), m, k, n, g, _ptr(offsets), _ptr(rows), _ptr(x), ldx,
-                                                _ptr(w), _ptr(dy), lddy, _ptr(dx), lddx, _ptr(dw), ws, ws_bytes,
-                                                _stream(stream, dev)))
-    return dx, dw
+            dw = torch.empty((g, k, n), dtype=dt, device=x.device)
+        dw_p = _whole(dw, "dw", (g, k, n), dt, index)
+        keep, ws, ws_bytes = _scratch(workspace, allegro_grouped_matmul_workspace(m, k, n, g), index)
+    _check(_lib.allegro_grouped_matmul_backward(code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, w_p, dy.data_ptr(),
+                                                lddy, dx_p, lddx, dw_p, ws, ws_bytes, _stream_of(stream, index)))
+    return dx if need_dx else None, dw if need_dw else None
 
 
 def allegro_grouped_matmul_fp8(x, x_scale, w, w_scale, offsets=None, rows=None, out=None, stream=None):
-    """Returns y [M, N] bfloat16 from float8_e4m3fn x [M, K] with x_scale [M, ceil(K/128)] and float8_e4m3fn w [G, N, K] with
-    w_scale [G, ceil(N/128), ceil(K/128)].  Without offsets w has one group, of all rows."""
-    f8 = torch.float8_e4m3fn
-    m, k = _matrix(x, "x")
-    dev = x.device
-    g, n, wk = _groups(w, "N, K", offsets, rows, m, dev)
-    _need(w, "w", (g, n, k), f8, dev)
-    kb, nb = -(-k // SCALE_BLOCK), -(-n // SCALE_BLOCK)
-    _need(x_scale, "x_scale", (m, kb), torch.float32, dev)
-    _need(w_scale, "w_scale", (g, nb, kb), torch.float32, dev)
+    """Returns y [M, N] bfloat16 from float8_e4m3fn x [M, K] with x_scale [M, ceil(K/128)] and float8_e4m3fn w [G, N, K]
+    with w_scale [G, ceil(N/128), ceil(K/128)].  Without offsets w has one group, of all rows."""
+    if not isinstance(x, _Tensor):
+        raise TypeError("x must be a torch.Tensor")
+    index, shape = _index(x, "x"), x.shape
+    m, k = shape
+    g, n, _ = _weights(w, "N, K")
+    kb, nb = (k + SCALE_BLOCK - 1) // SCALE_BLOCK, (n + SCALE_BLOCK - 1) // SCALE_BLOCK
     if out is None:
-        out = torch.empty((m, n), dtype=torch.bfloat16, device=dev)
-    ldx, ldy = _rows(x, "x", (m, k), f8, dev), _rows(out, "out", (m, n), torch.bfloat16, dev)
-    _check(_lib.allegro_grouped_matmul_fp8(m, k, n, g, _ptr(offsets), _ptr(rows), _ptr(x), ldx, _ptr(x_scale),
-                                           _ptr(w), _ptr(w_scale), _ptr(out), ldy, _stream(stream, dev)))
+        out = torch.empty((m, n), dtype=_BF16, device=x.device)
+    w_p = _whole(w, "w", (g, n, k), _F8, index)
+    xs_p = _whole(x_scale, "x_scale", (m, kb), _F32, index)
+    ws_p = _whole(w_scale, "w_scale", (g, nb, kb), _F32, index)
+    o_p, r_p = _groups(offsets, rows, g, m, index)
+    ldx, ldy = _rows(x, "x", shape, _F8, index), _rows(out, "out", (m, n), _BF16, index)
+    _check(_lib.allegro_grouped_matmul_fp8(m, k, n, g, o_p, r_p, x.data_ptr(), ldx, xs_p, w_p, ws_p, out.data_ptr(),
+                                           ldy, _stream_of(stream, index)))
     return out
 
 
 # -------------------------------------------------------------------- norm
 
 def _norm_inputs(x, w, residual, total):
-    code = _dtype(x, "x")
-    m, c = _matrix(x, "x")
-    dev = x.device
-    _need(w, "w", (c,), torch.float32, dev)
-    ldx, ldr, ldt = _rows(x, "x", (m, c), x.dtype, dev), 0, 0
+    """(dtype code, device index, addresses and strides of x, residual, w and total, total)."""
+    code, index = _matrix(x, "x")
+    dt, shape = x.dtype, x.shape
+    w_p = _whole(w, "w", shape[1:], _F32, index)
+    ldx, r_p, ldr, t_p, ldt = _rows(x, "x", shape, dt, index), 0, 0, 0, 0
     if residual is not None:
-        ldr = _rows(residual, "residual", (m, c), x.dtype, dev)
+        ldr, r_p = _rows(residual, "residual", shape, dt, index), residual.data_ptr()
         if total is None:
-            total = torch.empty((m, c), dtype=x.dtype, device=dev)
+            total = torch.empty(shape, dtype=dt, device=x.device)
     if total is not None:
-        ldt = _rows(total, "total", (m, c), x.dtype, dev)
-    return code, m, c, dev, ldx, ldr, total, ldt
+        ldt, t_p = _rows(total, "total", shape, dt, index), total.data_ptr()
+    return code, index, (x.data_ptr(), ldx, r_p, ldr, w_p, t_p, ldt), total
 
 
 def allegro_rms_norm_forward(x, w, residual=None, eps: float = 1e-6, total=None, out=None, rstd=None, stream=None):
     """Returns (y [M, C], total [M, C], rstd [M]): total = x + residual (x itself without a residual), y = total *
     rstd * w with rstd = 1 / sqrt(mean(total^2) + eps).  total and rstd are what the backward takes."""
-    code, m, c, dev, ldx, ldr, total, ldt = _norm_inputs(x, w, residual, total)
+    code, index, args, total = _norm_inputs(x, w, residual, total)
+    shape, dt = x.shape, x.dtype
+    m, c = shape
     if out is None:
-        out = torch.empty((m, c), dtype=x.dtype, device=dev)
+        out = torch.empty(shape, dtype=dt, device=x.device)
     if rstd is None:
-        rstd = torch.empty(m, dtype=torch.float32, device=dev)
-    _need(rstd, "rstd", (m,), torch.float32, dev)
-    ldy = _rows(out, "out", (m, c), x.dtype, dev)
-    _check(_lib.allegro_rms_norm_forward(code, m, c, float(eps), _ptr(x), ldx, _ptr(residual), ldr, _ptr(w),
-                                         _ptr(total), ldt, _ptr(out), ldy, _ptr(rstd), _stream(stream, dev)))
+        rstd = torch.empty(m, dtype=_F32, device=x.device)
+    rstd_p, ldy = _whole(rstd, "rstd", (m,), _F32, index), _rows(out, "out", shape, dt, index)
+    _check(_lib.allegro_rms_norm_forward(code, m, c, eps, *args, out.data_ptr(), ldy, rstd_p,
+                                         _stream_of(stream, index)))
     return out, x if total is None else total, rstd
 
 
 def allegro_rms_norm_fp8(x, w, residual=None, eps: float = 1e-6, total=None, q=None, scale=None, stream=None):
     """Returns (q [M, C] float8_e4m3fn, scale [M, ceil(C/128)], total [M, C]): the norm as q * scale."""
-    code, m, c, dev, ldx, ldr, total, ldt = _norm_inputs(x, w, residual, total)
-    blocks = -(-c // SCALE_BLOCK)
+    code, index, args, total = _norm_inputs(x, w, residual, total)
+    shape = x.shape
+    m, c = shape
+    blocks = (c + SCALE_BLOCK - 1) // SCALE_BLOCK
     if q is None:
-        q = torch.empty((m, c), dtype=torch.float8_e4m3fn, device=dev)
+        q = torch.empty(shape, dtype=_F8, device=x.device)
     if scale is None:
-        scale = torch.empty((m, blocks), dtype=torch.float32, device=dev)
-    _need(scale, "scale", (m, blocks), torch.float32, dev)
-    ldq = _rows(q, "q", (m, c), torch.float8_e4m3fn, dev)
-    _check(_lib.allegro_rms_norm_fp8(code, m, c, float(eps), _ptr(x), ldx, _ptr(residual), ldr, _ptr(w), _ptr(total),
-                                     ldt, _ptr(q), ldq, _ptr(scale), _stream(stream, dev)))
+        scale = torch.empty((m, blocks), dtype=_F32, device=x.device)
+    scale_p, ldq = _whole(scale, "scale", (m, blocks), _F32, index), _rows(q, "q", shape, _F8, index)
+    _check(_lib.allegro_rms_norm_fp8(code, m, c, eps, *args, q.data_ptr(), ldq, scale_p, _stream_of(stream, index)))
     return q, scale, x if total is None else total
 
 
 def allegro_rms_norm_workspace(n_rows: int, c: int) -> int:
     """Bytes of workspace allegro_rms_norm_backward needs."""
-    out = ctypes.c_size_t()
-    _check(_lib.allegro_rms_norm_workspace(int(n_rows), int(c), ctypes.byref(out)))
-    return out.value
+    return _bytes(_lib.allegro_rms_norm_workspace, n_rows, c)
 
 
 def allegro_rms_norm_backward(total, w, rstd, dy, dtotal=None, dx=None, dw=None, workspace=None, stream=None):
     """Returns (dx [M, C], dw [C]): dx is the gradient of x and of the residual alike, with dtotal, the gradient
     that reaches total along the residual, added."""
-    code = _dtype(total, "total")
-    m, c = _matrix(total, "total")
-    dev, dt = total.device, total.dtype
-    _need(w, "w", (c,), torch.float32, dev)
-    _need(rstd, "rstd", (m,), torch.float32, dev)
-    ldt, lddy = _rows(total, "total", (m, c), dt, dev), _rows(dy, "dy", (m, c), dt, dev)
-    lddt = 0 if dtotal is None else _rows(dtotal, "dtotal", (m, c), dt, dev)
+    code, index = _matrix(total, "total")
+    dt, shape = total.dtype, total.shape
+    m, c = shape
+    w_p, rstd_p = _whole(w, "w", (c,), _F32, index), _whole(rstd, "rstd", (m,), _F32, index)
+    ldt, lddy = _rows(total, "total", shape, dt, index), _rows(dy, "dy", shape, dt, index)
+    ds_p, ldds = 0, 0
+    if dtotal is not None:
+        ldds, ds_p = _rows(dtotal, "dtotal", shape, dt, index), dtotal.data_ptr()
     if dx is None:
-        dx = torch.empty((m, c), dtype=dt, device=dev)
+        dx = torch.empty(shape, dtype=dt, device=total.device)
     if dw is None:
-        dw = torch.empty(c, dtype=torch.float32, device=dev)
-    _need(dw, "dw", (c,), torch.float32, dev)
-    lddx = _rows(dx, "dx", (m, c), dt, dev)
-    ws, ws_bytes = _scratch(workspace, allegro_rms_norm_workspace(m, c), dev)
-    _check(_lib.allegro_rms_norm_backward(code, m, c, _ptr(total), ldt, _ptr(w), _ptr(rstd), _ptr(dy), lddy,
-                                          _ptr(dtotal), lddt, _ptr(dx), lddx, _ptr(dw), ws, ws_bytes,
-                                          _stream(stream, dev)))
+        dw = torch.empty(c, dtype=_F32, device=total.device)
+    dw_p, lddx = _whole(dw, "dw", (c,), _F32, index), _rows(dx, "dx", shape, dt, index)
+    keep, ws, ws_bytes = _scratch(workspace, allegro_rms_norm_workspace(m, c), index)
+    _check(_lib.allegro_rms_norm_backward(code, m, c, total.data_ptr(), ldt, w_p, rstd_p, dy.data_ptr(), lddy, ds_p, ldds,
+                                          dx.data_ptr(), lddx, dw_p, ws, ws_bytes, _stream_of(stream, index)))
     return dx, dw
