@@ -41,17 +41,17 @@
  *   value 448 ("e4m3fn").  Sums, norms and statistics are held in fp32 and
  *   rounded to dtype once, when an output is written; with ALLEGRO_BF16 the
  *   products round act(X) to bf16 as their operand when act is SiLU.  fp32
- *   products keep fp32 accuracy, 8-bit ones that of their bf16 output.  Infinities and NaN propagate as in the
- *   formulas.
+ *   products keep fp32 accuracy, 8-bit ones that of their bf16 output.
+ *   Infinities and NaN propagate as in the formulas.
  *
  * Memory and ownership
  *   Tensors are caller-owned device memory.  A tensor of rows has unit column
  *   stride and the row stride given with it, in elements and at least its
  *   width; W, dW, w, dw, rstd, scales, offsets and rows are contiguous.
- *   Pointers are aligned to their element; 16-byte aligned rows (pointer, row
- *   stride and width) take the fast paths.  Outputs are overwritten and alias
- *   nothing.  Workspaces are 16-byte aligned and hold nothing between calls;
- *   calls that share one must not overlap.  Nothing is allocated per call.
+ *   Pointers are aligned to their element; nothing more is asked of pointers,
+ *   strides and widths, and all take the same kernels.  Outputs are overwritten
+ *   and alias nothing.  Workspaces are 16-byte aligned and hold nothing between
+ *   calls; calls that share one must not overlap.  Nothing is allocated per call.
  *
  *   offsets and rows are read on the device: offsets out of order or range and
  *   rows outside 0 .. M-1 cause no access out of bounds, but the outputs of the

@@ -57,10 +57,6 @@ inline int after(const char *what) {
   return e == hipSuccess ? ALLEGRO_OK : fail(ALLEGRO_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-inline bool aligned(const void *p, int64_t stride_bytes, int to) {
-  return reinterpret_cast<uintptr_t>(p) % unsigned(to) == 0 && stride_bytes % to == 0;
-}
-
 // Host checks.  A tensor of rows: pointer, element alignment, row stride.
 inline int check_ptr(const void *p, const char *name, int elem) {
   if (!p) return fail(ALLEGRO_E_INVALID, "%s is NULL", name);

@@ -8,12 +8,11 @@
 //   product_f8_kernel  the 8-bit product
 //
 // Ragged groups.  The offsets are on the device, so the host launches an upper
-// bound of tiles: group g's tiles start at index (offsets[g] >> shift) + g.  A
-// group of n rows needs at most (n >> shift) + 2 tiles less whatever the next
-// group's start rounds off, which is what that index leaves room for, so every
-// workgroup finds its group by comparing its index with those of all groups,
-// with no sums over groups and no launch before.  Rows without a type are one
-// more group, of zeros.
+// bound of tiles, (M >> shift) + G + 1, and a workgroup finds its tile by itself:
+// group g's tiles are numbered from (offsets[g] >> shift) + g on.  Rounding down
+// loses less than one tile per group and + g gives one back, so a group's tiles
+// never reach the next one's number.  No sums over groups and no launch go before;
+// rows without a type are one more group, of zeros.
 //
 // Operands.  Every tensor is read 16 bytes at a time along its memory rows.  Where
 // the contraction runs along them (X and, transposed, W) a tile lies in LDS as it
@@ -223,8 +222,9 @@ __device__ __forceinline__ int swizzled(int r, int c) {
 // A tile of `ROWS` rows (of X, or columns of the result) whose contraction runs
 // along memory.  In LDS: rows of KS 16-bit values, in 16-byte chunks swizzled by
 // row so that 8 and 16 lanes reading one chunk of consecutive rows hit distinct
-// banks.  NT threads move pieces tid % 8 of rows tid / 8 + RP i.
-template <class T, int ROWS, bool WIDE, int NT = kThreads>
+// banks.  NT threads move pieces tid % 8 of rows tid / 8 + RP i.  SHORT as in
+// load_pieces: without it every row must have PE elements.
+template <class T, int ROWS, bool WIDE, int NT, bool SHORT>
 struct Along {
   static constexpr int P = Kind<T>::P, KS = Kind<T>::KS, PE = Kind<T>::PE, RP = NT / 8, NP = ROWS / RP, C = KS / 8;
   static constexpr int SIZE = P * ROWS * C;  // 16-byte units
@@ -233,7 +233,7 @@ struct Along {
   // row(i): pointer to the first element of row row(i, tid); n elements to a row
   template <class Row>
   __device__ __forceinline__ void load(Row row, int k0, int n, int tid) {
-    load_pieces<T, NT == kThreads>(v, row, k0 + PE * (tid % 8), n);
+    load_pieces<T, SHORT>(v, row, k0 + PE * (tid % 8), n);
   }
   __device__ __forceinline__ void put(u32x4 *lds, bool act, float scale, int k0, int n, int tid) {
     if (k0 + KS > n) {  // the last step: nothing from n on
@@ -277,7 +277,7 @@ struct Along {
 // LDS load, by which 16 lanes turn 4 rows of 16 columns into 4 rows of one column
 // each.  A wave's load touches 4 columns' quads of 16 rows; chunks (and their
 // halves) are swizzled by row so that those 512 bytes lie in all banks twice.
-template <class T, int COLS, bool WIDE, int NT = kThreads>
+template <class T, int COLS, bool WIDE, int NT, bool SHORT>
 struct Across {
   static constexpr int P = Kind<T>::P, KS = Kind<T>::KS, PE = Kind<T>::PE;
   static constexpr int PR = COLS / PE, RP = NT / PR, NP = KS / RP;  // pieces to a row, rows to a pass
@@ -293,7 +293,7 @@ struct Across {
   // columns start at c0 of n
   template <class Row>
   __device__ __forceinline__ void load(Row row, int c0, int n, int tid) {
-    load_pieces<T, NT == kThreads>(v, row, c0 + col(tid), n);
+    load_pieces<T, SHORT>(v, row, c0 + col(tid), n);
   }
   // missing: bit i is set if step(i, tid) does not exist and becomes zero
   __device__ __forceinline__ void put(u32x4 *lds, bool act, float scale, int c0, int n, int missing, int tid) {
@@ -542,14 +542,18 @@ struct ProductArgs {
 // Threads of a tile TN columns wide: four waves, or eight of a wide one, each with
 // 64 rows and 32 or 64 columns.
 constexpr int tile_threads(int TN) { return TN == 256 ? 2 * kThreads : kThreads; }
+// Whether K or N may be less than a 16-byte piece: tiles of 256 columns are launched
+// with K > 64 and N > 128 only.
+constexpr bool tile_short(int TN) { return TN != 256; }
 
 template <class T, int TN, bool WT>
 __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void product_kernel(ProductArgs g) {
   constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NT = tile_threads(TN), MI = 4, NI = TN / (NT / 128) / 16;
-  using XTile = Along<T, kTileRows, false, NT>;
-  using WTile = std::conditional_t<WT, Along<T, TN, !F32, NT>, Across<T, TN, !F32, NT>>;
+  using XTile = Along<T, kTileRows, false, NT, tile_short(TN)>;
+  using WTile = std::conditional_t<WT, Along<T, TN, !F32, NT, tile_short(TN)>,
+                                   Across<T, TN, !F32, NT, tile_short(TN)>>;
   __shared__ u32x4 x_lds[XTile::SIZE], w_lds[WTile::SIZE];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
@@ -725,7 +729,7 @@ __device__ __forceinline__ void stream_zeros(int chunks, List list, T *y, int64_
 template <int TN, bool WT>
 __global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(ProductArgs g) {
   constexpr int KS = Kind<float>::KS, PE = Kind<float>::PE, XP = 8 / PE, MT = 2, NI = TN / 16, RB = 16 * MT;
-  using WTile = std::conditional_t<WT, Along<float, TN, false>, Across<float, TN, false>>;
+  using WTile = std::conditional_t<WT, Along<float, TN, false, kThreads, true>, Across<float, TN, false, kThreads, true>>;
   __shared__ u32x4 w_lds[kStreamLds / 16];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
@@ -960,8 +964,8 @@ __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void weight_ke
   constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NT = tile_threads(TN), MI = TK / 32, NI = TN / (NT / 128) / 16;
-  using XTile = Across<T, TK, false, NT>;
-  using YTile = Across<T, TN, false, NT>;
+  using XTile = Across<T, TK, false, NT, tile_short(TN)>;
+  using YTile = Across<T, TN, false, NT, tile_short(TN)>;
   __shared__ u32x4 x_lds[XTile::SIZE], y_lds[YTile::SIZE];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int tiles = g.kt * g.nt;
@@ -1562,16 +1566,16 @@ void launch_weight(WeightArgs g, const WeightShape &z, hipStream_t s) {
     // against 23, 32,000 66 against 57, 400,000 584 against 445 and 497 against 484
     if (wide) hipLaunchKernelGGL((weight_kernel<T, 128, 256>), grid, dim3(tile_threads(256)), 0, s, g);
   }
-  if (wide)
-    ;
-  else if (g.K <= 64 && g.N <= 64)
-    hipLaunchKernelGGL((weight_kernel<T, 64, 64>), grid, block, 0, s, g);
-  else if (g.K <= 64)
-    hipLaunchKernelGGL((weight_kernel<T, 64, 128>), grid, block, 0, s, g);
-  else if (g.N <= 64)
-    hipLaunchKernelGGL((weight_kernel<T, 128, 64>), grid, block, 0, s, g);
-  else
-    hipLaunchKernelGGL((weight_kernel<T, 128, 128>), grid, block, 0, s, g);
+  if (!wide) {
+    if (g.K <= 64 && g.N <= 64)
+      hipLaunchKernelGGL((weight_kernel<T, 64, 64>), grid, block, 0, s, g);
+    else if (g.K <= 64)
+      hipLaunchKernelGGL((weight_kernel<T, 64, 128>), grid, block, 0, s, g);
+    else if (g.N <= 64)
+      hipLaunchKernelGGL((weight_kernel<T, 128, 64>), grid, block, 0, s, g);
+    else
+      hipLaunchKernelGGL((weight_kernel<T, 128, 128>), grid, block, 0, s, g);
+  }
   if (z.slots) {
     const unsigned several = unsigned(std::min<int64_t>(g.G, g.M >> z.shift));
     const int64_t parts = cdiv(int64_t(g.K) * g.N, 256);
