@@ -539,22 +539,31 @@ struct ProductArgs {
   int64_t mt;  // upper bound of the row tiles
 };
 
-// Threads of a tile TN columns wide: four waves, or eight of a wide one, each with
-// 64 rows and 32 or 64 columns.
+// Threads of a tile TN columns wide: four waves, eight of a wide one.
 constexpr int tile_threads(int TN) { return TN == 256 ? 2 * kThreads : kThreads; }
 // Whether K or N may be less than a 16-byte piece: tiles of 256 columns are launched
 // with K > 64 and N > 128 only.
 constexpr bool tile_short(int TN) { return TN != 256; }
 
-template <class T, int TN, bool WT>
-__global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void product_kernel(ProductArgs g) {
+// A contraction step is loaded into registers, put into LDS as operands and
+// multiplied.  BUFS == 1: one step in LDS and two meetings of the waves a step;
+// several workgroups on a compute unit overlap each other's phases.  BUFS == 2, for
+// grids with a tile or two to a compute unit: eight waves and two steps in LDS, so
+// that the waves meet once a step and half of them put the next one while the others
+// multiply.
+template <class T, int TN, bool WT, int BUFS>
+__global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 && BUFS == 1 ? 4 : 2) void product_kernel(
+    ProductArgs g) {
   constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int NT = tile_threads(TN), MI = 4, NI = TN / (NT / 128) / 16;
+  // waves along the tile's rows; products of a wave
+  constexpr int NT = BUFS == 2 ? 512 : tile_threads(TN), WM = NT == 512 && TN == 64 ? 4 : 2;
+  constexpr int MI = 8 / WM, NI = TN / 16 / (NT / kWave / WM);
+  constexpr bool TIGHT = TN == 256 && BUFS == 1;  // 128 registers, for two workgroups of eight waves
   using XTile = Along<T, kTileRows, false, NT, tile_short(TN)>;
   using WTile = std::conditional_t<WT, Along<T, TN, !F32, NT, tile_short(TN)>,
                                    Across<T, TN, !F32, NT, tile_short(TN)>>;
-  __shared__ u32x4 x_lds[XTile::SIZE], w_lds[WTile::SIZE];
+  __shared__ u32x4 x_lds[BUFS * XTile::SIZE], w_lds[BUFS * WTile::SIZE];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
@@ -579,7 +588,7 @@ __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void product_k
   WTile bw;
   auto load = [&](int k0) {
     int t = tid;
-    if constexpr (TN == 256) asm volatile("" : "+v"(t));  // addresses are formed anew: 128 registers
+    if constexpr (TIGHT) asm volatile("" : "+v"(t));  // addresses are formed anew
     a.load([&](int i) { return x + int64_t(xr[i]) * g.ldx; }, k0, K, t);
     if constexpr (WT) {
       bw.load(
@@ -602,27 +611,46 @@ __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void product_k
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int wm = 64 * (wave % 2), wn = 16 * NI * (wave / 2);
+  const int wm = 16 * MI * (wave % WM), wn = 16 * NI * (wave / WM);
   const typename XTile::Reader x_read(wm / 16, l);
   const typename WTile::Reader w_read(wn / 16, l);
   const float xs = (tid / 8) % 2 ? -kScale : kScale;  // odd rows negated
-  load(0);
-  for (int k0 = 0; k0 < K; k0 += KS) {
-    lds_sync<NT / kWave>();  // the previous step has been read
-    a.put(x_lds, !WT && g.act, xs, k0, K, tid);
+  auto put = [&](int buf, int k0) {
+    a.put(x_lds + buf * XTile::SIZE, !WT && g.act, xs, k0, K, tid);
+    u32x4 *w_at = w_lds + buf * WTile::SIZE;
     if constexpr (WT) {
-      bw.put(w_lds, false, kScale, k0, K, tid);
+      bw.put(w_at, false, kScale, k0, K, tid);
     } else {
       int missing = 0;
       if (k0 + KS > K) {
 #pragma unroll
         for (int i = 0; i < WTile::NP; ++i) missing |= (k0 + WTile::step(i, tid) >= K) << i;
       }
-      bw.put(w_lds, false, kScale, n0, N, missing, tid);
+      bw.put(w_at, false, kScale, n0, N, missing, tid);
     }
-    lds_sync<NT / kWave>();
-    if (k0 + KS < K) load(k0 + KS);
-    multiply<T, XTile, WTile, TN == 256>(x_lds, w_lds, x_read, w_read, 1.f, acc);
+  };
+  load(0);
+  if constexpr (BUFS == 1) {
+    for (int k0 = 0; k0 < K; k0 += KS) {
+      lds_sync<NT / kWave>();  // the previous step has been read
+      put(0, k0);
+      lds_sync<NT / kWave>();
+      if (k0 + KS < K) load(k0 + KS);
+      multiply<T, XTile, WTile, TIGHT>(x_lds, w_lds, x_read, w_read, 1.f, acc);
+    }
+  } else {
+    put(0, 0);
+    if (KS < K) load(KS);
+    for (int k0 = 0, buf = 0; k0 < K; k0 += KS, buf ^= 1) {
+      lds_sync<NT / kWave>();  // this step is in LDS, and the one before has been read
+      auto next = [&] {
+        if (k0 + KS < K) put(buf ^ 1, k0 + KS);
+        if (k0 + 2 * KS < K) load(k0 + 2 * KS);
+      };
+      if (wave < NT / kWave / 2) next();
+      multiply<T, XTile, WTile, TIGHT>(x_lds + buf * XTile::SIZE, w_lds + buf * WTile::SIZE, x_read, w_read, 1.f, acc);
+      if (wave >= NT / kWave / 2) next();
+    }
   }
   if constexpr (F32) {
     if (any_not_finite(acc)) {
@@ -1509,27 +1537,45 @@ void launch_product(ProductArgs g, hipStream_t s) {
   }
   g.mt = tile_bound(g.M, g.G, kTileShift);
   if constexpr (sizeof(T) == 2 && !WT) {
-    // 256 columns at a time, so that a row's SiLU is computed half as often: K = 512,
-    // N = 512, us, 1 and 100 types: M = 32,000 38 against 29 and 50 against 46,
-    // M = 400,000 394 against 352 and 415 against 358; K = 1024 and one type 68
-    // against 49; M = 2,000 16 against 19.  Without SiLU and for the gradient of X
-    // both are within 5%.
-    if (g.act && g.N > 128 && g.K >= 256 && g.M >= 16384) {
-      g.nt = int(cdiv(g.N, 256));
-      hipLaunchKernelGGL((product_kernel<T, 256, false>), dim3(unsigned(g.mt * g.nt)), dim3(tile_threads(256)), 0, s, g);
+    // 256 columns at a time, so that a row's SiLU is computed half as often: against
+    // 128, K = 512, N = 512, 1 and 100 types: M = 32,000 38 against 29 and 50 against
+    // 46, M = 400,000 394 against 352 and 415 against 358; against 64, M = 3,700 and 100
+    // types 28 against 19.  Without SiLU and for the gradient of X both are within 5%.
+    // Two buffers up to a tile per compute unit: 204 tiles, K = 1024 35 against 28;
+    // 254, K = 512 22 against 18; 259, K = 1024 46 against 50.
+    const int nt = int(cdiv(g.N, 256));
+    const int64_t tiles = g.mt * nt;
+    if (g.act && g.N > 128 && g.K >= 256 && tiles > 128) {
+      g.nt = nt;
+      const dim3 grid{unsigned(tiles)}, block(2 * kThreads);
+      if (tiles <= 256)
+        hipLaunchKernelGGL((product_kernel<T, 256, false, 2>), grid, block, 0, s, g);
+      else
+        hipLaunchKernelGGL((product_kernel<T, 256, false, 1>), grid, block, 0, s, g);
       return;
     }
   }
   // 64 columns at a time where 128 would leave compute units without a tile, or a
-  // quarter of the columns empty: fp32, 16 types, us, M = 3,700 K = 192 N = 128 19
-  // against 15, K = 1024 N = 256 81 against 64; the gradient of X also gains with up to
-  // two tiles to a unit (M = 3,700 512 x 512 44 against 37, bf16 14 against 12.4)
+  // quarter of the columns empty: 128 against 64, forward of fp32 512 x 512: 164 tiles
+  // (of 128 columns) 39 against 31, 316 53 against 51, 424 55 against 62; bf16 17 against
+  // 15 and 17.5 against 17.9 at 316 and 424.  The gradient of X gains with more tiles:
+  // fp32 K = 256, N = 256 530 tiles 55 against 44, K = 768, N = 128 636 tiles 41 against
+  // 32, 512 x 512 756 tiles 90 and 90; bf16 474 tiles 12.6 against 11.5, 530 17.6
+  // against 18.2.  Two buffers against one, forward: fp32 M = 5,000 K = 768, N = 128 41
+  // against 29, M = 50,000 256 x 64 28 against 25; bf16 M = 3,700 1024 x 256 22.3
+  // against 20.0, but with 1,564 tiles of 64 x 64 13.8 against 16.4.
+  constexpr bool F32 = sizeof(T) == 4;
   const int64_t tiles = g.mt * g.nt;
-  if (narrow || tiles <= (WT ? 512 : 128) || 4 * g.N <= 3 * 128 * g.nt) {
+  if (narrow || tiles <= (!WT ? 320 : F32 ? 640 : 512) || 4 * g.N <= 3 * 128 * g.nt) {
     g.nt = int(cdiv(g.N, 64));
-    hipLaunchKernelGGL((product_kernel<T, 64, WT>), dim3(unsigned(g.mt * g.nt)), dim3(kThreads), 0, s, g);
+    const dim3 grid{unsigned(g.mt * g.nt)};
+    if (F32 || grid.x <= 256) {
+      hipLaunchKernelGGL((product_kernel<T, 64, WT, 2>), grid, dim3(2 * kThreads), 0, s, g);
+      return;
+    }
+    if constexpr (!F32) hipLaunchKernelGGL((product_kernel<T, 64, WT, 1>), grid, dim3(kThreads), 0, s, g);
   } else {
-    hipLaunchKernelGGL((product_kernel<T, 128, WT>), dim3(unsigned(tiles)), dim3(kThreads), 0, s, g);
+    hipLaunchKernelGGL((product_kernel<T, 128, WT, 1>), dim3(unsigned(tiles)), dim3(kThreads), 0, s, g);
   }
 }
 
