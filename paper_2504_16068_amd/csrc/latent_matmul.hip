@@ -8,8 +8,8 @@
 //   product_f8_kernel  the 8-bit product
 //
 // Ragged groups.  The offsets are on the device, so the host launches an upper
-// bound of tiles, (M >> shift) + G + 1, and a workgroup finds its tile by itself:
-// group g's tiles are numbered from (offsets[g] >> shift) + g on.  Rounding down
+// bound of tiles, M / rows + G + 1, and a workgroup finds its tile by itself: group
+// g's tiles of `rows` rows are numbered from offsets[g] / rows + g on.  Rounding down
 // loses less than one tile per group and + g gives one back, so a group's tiles
 // never reach the next one's number.  No sums over groups and no launch go before;
 // rows without a type are one more group, of zeros.
@@ -36,7 +36,7 @@ using allegro_dev::lds_sync;
 using allegro_dev::static_for;
 
 constexpr int kThreads = 256;
-constexpr int kTileRows = 128, kTileShift = 7;  // rows of a tile
+constexpr int kTileRows = 128;  // rows of a tile
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
@@ -59,19 +59,19 @@ struct Tile {
   int64_t begin, m0, end;  // list positions: the group, the tile's first row; nothing to do if m0 >= end
 };
 
-__device__ __forceinline__ Tile find_tile(const int64_t *__restrict__ offsets, int G, int64_t M, int shift, int64_t t,
-                                          int lane) {
+__device__ __forceinline__ Tile find_tile(const int64_t *__restrict__ offsets, int G, int64_t M, uint32_t rows,
+                                          int64_t t, int lane) {
   auto clamped = [&](int i) {
     const int64_t o = offsets[i];
     return o < 0 ? int64_t(0) : o > M ? M : o;
   };
   int below = 0;
-  for (int i = lane; i <= G; i += kWave) below += (clamped(i) >> shift) + i <= t;
+  for (int i = lane; i <= G; i += kWave) below += uint32_t(clamped(i)) / rows + int64_t(i) <= t;
   for (int m = kWave / 2; m; m >>= 1) below += __shfl_xor(below, m);
   const int g = __builtin_amdgcn_readfirstlane(below > 0 ? below - 1 : 0);
   const int64_t begin = clamped(g), end = g < G ? clamped(g + 1) : M;
-  const int64_t k = t - ((begin >> shift) + g);
-  return {g, begin, k < 0 ? end : begin + (k << shift), end};
+  const int64_t k = t - (uint32_t(begin) / rows + int64_t(g));
+  return {g, begin, k < 0 ? end : begin + k * rows, end};
 }
 
 // The group at `unit` of a line on which group g starts at offsets[g] + cost * g.
@@ -89,7 +89,7 @@ __device__ __forceinline__ Tile find_group(const int64_t *__restrict__ offsets, 
   return {g, begin, begin, end > begin ? end : begin};
 }
 
-__host__ __device__ inline int64_t tile_bound(int64_t M, int G, int shift) { return (M >> shift) + G + 1; }
+__host__ __device__ inline int64_t tile_bound(int64_t M, int G, int rows) { return M / rows + G + 1; }
 
 // Workgroups go round the 8 XCDs: give each XCD consecutive tiles, so that the
 // tiles that share rows or weights share an L2.
@@ -567,7 +567,7 @@ __global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 && BU
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
-  const Tile t = find_tile(g.offsets, g.G, g.M, kTileShift, b / g.nt, l);
+  const Tile t = find_tile(g.offsets, g.G, g.M, kTileRows, b / g.nt, l);
   if (t.m0 >= t.end) return;
   const int n0 = int(b % g.nt) * TN, K = g.K, N = g.N;
   T *y = static_cast<T *>(g.y);
@@ -971,7 +971,7 @@ __global__ __launch_bounds__(kStreamThreads, 2) void product_stream_kernel(Produ
 // ------------------------------------------------------- weight gradient
 struct WeightArgs {
   int64_t M;
-  int K, N, G, act, shift;  // ranges of 1 << shift rows
+  int K, N, G, act, range;  // rows of a range
   const int64_t *offsets;
   const int32_t *rows;
   const void *x;  // [M][K]
@@ -979,33 +979,37 @@ struct WeightArgs {
   const void *dy;  // [M][N]
   int64_t lddy;
   void *dw;     // [G][K][N]
-  float *part;  // [2 (M >> shift) + 1][slot]
+  float *part;  // [2 (M / range) + 1][slot]
   int64_t slot;
   int kt, nt;
   int64_t ranges;  // upper bound
 };
 
-// Range k of a group of several goes to slot 2 (offsets[g] >> shift) + k: such a
-// group has more than 1 << shift rows, so the next one's slots start behind it.
-template <class T, int TK, int TN>
-__global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void weight_kernel(WeightArgs g) {
+// Range k of a group of several goes to slot 2 (offsets[g] / range) + k: such a
+// group has more than `range` rows, so the next one's slots start behind it.  BUFS as
+// in product_kernel.
+template <class T, int TK, int TN, int BUFS>
+__global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 ? 4 : 2) void weight_kernel(
+    WeightArgs g) {
   constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int NT = tile_threads(TN), MI = TK / 32, NI = TN / (NT / 128) / 16;
+  // waves along the rows of dW; products of a wave
+  constexpr int NT = BUFS == 2 ? 512 : tile_threads(TN), WK = BUFS == 2 && TK > TN ? 4 : 2;
+  constexpr int MI = TK / 16 / WK, NI = TN / 16 / (NT / kWave / WK);
   using XTile = Across<T, TK, false, NT, tile_short(TN)>;
   using YTile = Across<T, TN, false, NT, tile_short(TN)>;
-  __shared__ u32x4 x_lds[XTile::SIZE], y_lds[YTile::SIZE];
+  __shared__ u32x4 x_lds[BUFS * XTile::SIZE], y_lds[BUFS * YTile::SIZE];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
   const int tiles = g.kt * g.nt;
   // in plain order over the XCDs: groups differ in length, and a range's tiles
   // take the same time
   const int64_t b = blockIdx.x;
-  const Tile t = find_tile(g.offsets, g.G, g.M, g.shift, b / tiles, l);
+  const Tile t = find_tile(g.offsets, g.G, g.M, g.range, b / tiles, l);
   if (t.g == g.G) return;
   const int64_t begin = t.begin;
-  const bool only = t.end - begin <= (int64_t(1) << g.shift);  // the group's only range, if it has rows at all
+  const bool only = t.end - begin <= g.range;  // the group's only range, if it has rows at all
   if (t.m0 >= t.end && !(t.m0 == begin && t.end == begin)) return;
-  const int64_t end = t.m0 + (int64_t(1) << g.shift) < t.end ? t.m0 + (int64_t(1) << g.shift) : t.end;
+  const int64_t end = t.m0 + g.range < t.end ? t.m0 + g.range : t.end;
   const int k0 = int(b % tiles) / g.nt * TK, n0 = int(b % tiles) % g.nt * TN, K = g.K, N = g.N;
   const T *x = static_cast<const T *>(g.x), *dy = static_cast<const T *>(g.dy);
   auto row_of = [&](int64_t i) -> int {
@@ -1041,7 +1045,7 @@ __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void weight_ke
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int wk = TK / 2 * (wave % 2), wn = 16 * NI * (wave / 2);
+  const int wk = 16 * MI * (wave % WK), wn = 16 * NI * (wave / WK);
   const typename XTile::Reader x_read(wk / 16, l);
   const typename YTile::Reader y_read(wn / 16, l);
   float sign = 1.f;
@@ -1050,17 +1054,44 @@ __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void weight_ke
     load();
     rows = row_of(t.m0 + KS + l % KS);
   }
-  for (int64_t m = t.m0; m < end; m += KS) {
-    lds_sync<NT / kWave>();
-    xa.put(x_lds, g.act, sign * kScale, k0, K, xm, tid);
-    ya.put(y_lds, false, kScale, n0, N, ym, tid);
-    lds_sync<NT / kWave>();
-    if (m + KS < end) {
-      load();
-      rows = row_of(m + 2 * KS + l % KS);
+  auto put = [&](int buf, float sign) {
+    xa.put(x_lds + buf * XTile::SIZE, g.act, sign * kScale, k0, K, xm, tid);
+    ya.put(y_lds + buf * YTile::SIZE, false, kScale, n0, N, ym, tid);
+  };
+  if constexpr (BUFS == 1) {
+    for (int64_t m = t.m0; m < end; m += KS) {
+      lds_sync<NT / kWave>();
+      put(0, sign);
+      lds_sync<NT / kWave>();
+      if (m + KS < end) {
+        load();
+        rows = row_of(m + 2 * KS + l % KS);
+      }
+      multiply<T, XTile, YTile, TN == 256>(x_lds, y_lds, x_read, y_read, sign, acc);
+      sign = -sign;
     }
-    multiply<T, XTile, YTile, TN == 256>(x_lds, y_lds, x_read, y_read, sign, acc);
-    sign = -sign;
+  } else if (t.m0 < end) {
+    put(0, sign);
+    if (t.m0 + KS < end) {
+      load();
+      rows = row_of(t.m0 + 2 * KS + l % KS);
+    }
+    int buf = 0;
+    for (int64_t m = t.m0; m < end; m += KS) {
+      lds_sync<NT / kWave>();
+      auto next = [&] {
+        if (m + KS < end) put(buf ^ 1, -sign);
+        if (m + 2 * KS < end) {
+          load();
+          rows = row_of(m + 3 * KS + l % KS);
+        }
+      };
+      if (wave < NT / kWave / 2) next();
+      multiply<T, XTile, YTile, TN == 256>(x_lds + buf * XTile::SIZE, y_lds + buf * YTile::SIZE, x_read, y_read, sign, acc);
+      if (wave >= NT / kWave / 2) next();
+      sign = -sign;
+      buf ^= 1;
+    }
   }
   if constexpr (F32) {
     if (any_not_finite(acc)) {
@@ -1084,7 +1115,7 @@ __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void weight_ke
         for (int j = 0; j < NI; ++j) acc[i][j] *= kUnscale;
     }
   }
-  const int64_t k_first = (t.m0 - begin) >> g.shift;
+  const int k_first = uint32_t(t.m0 - begin) / uint32_t(g.range);
 #pragma unroll
   for (int i = 0; i < MI; ++i) {
     const int k = k0 + wk + 16 * i + l % 16;
@@ -1098,7 +1129,7 @@ __global__ __launch_bounds__(tile_threads(TN), TN == 256 ? 4 : 2) void weight_ke
       if (only)
         store_row<4>(static_cast<T *>(g.dw) + (int64_t(t.g) * K + k) * N + n, v, N - n);
       else
-        store_row<4>(g.part + (2 * (begin >> g.shift) + k_first) * g.slot + int64_t(k) * N + n, v, N - n);
+        store_row<4>(g.part + (2 * int64_t(uint32_t(begin) / uint32_t(g.range)) + k_first) * g.slot + int64_t(k) * N + n, v, N - n);
     }
   }
 }
@@ -1119,7 +1150,7 @@ __global__ __launch_bounds__(kSumThreads) void weight_sum_kernel(WeightArgs g) {
   int left = blockIdx.y, found = -1;
   for (int i0 = 0; i0 < g.G && found < 0; i0 += kWave) {
     const int i = i0 + l;
-    const uint64_t several = __ballot(i < g.G && clamped(i + 1) - clamped(i) > (int64_t(1) << g.shift));
+    const uint64_t several = __ballot(i < g.G && clamped(i + 1) - clamped(i) > g.range);
     const int n = __popcll(several);
     if (left < n) {
       uint64_t rest = several;
@@ -1131,12 +1162,12 @@ __global__ __launch_bounds__(kSumThreads) void weight_sum_kernel(WeightArgs g) {
   }
   if (found < 0) return;
   const int64_t begin = clamped(found), rows = clamped(found + 1) - begin, KN = int64_t(g.K) * g.N;
-  const int ranges = int((rows + (int64_t(1) << g.shift) - 1) >> g.shift);
+  const int ranges = int((rows + g.range - 1) / g.range);
   const int64_t e = (SPLIT ? int64_t(blockIdx.x) : int64_t(blockIdx.x) * kSumWaves + wave) * 256 + 4 * l;
   const int first = SPLIT ? wave : 0, step = SPLIT ? kSumWaves : 1;
   f32x4 s = {0.f, 0.f, 0.f, 0.f};
   if (e < KN) {
-    const float *p = g.part + 2 * (begin >> g.shift) * g.slot + e;  // slots are padded to whole vectors
+    const float *p = g.part + 2 * (begin / g.range) * g.slot + e;  // slots are padded to whole vectors
 #pragma unroll 8
     for (int k = first; k < ranges; k += step) s += *reinterpret_cast<const f32x4 *>(p + k * g.slot);
   }
@@ -1214,9 +1245,9 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
   const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
   Tile t;
   if (g.offsets)
-    t = find_tile(g.offsets, g.G, g.M, kTileShift, b / g.nt, l);
+    t = find_tile(g.offsets, g.G, g.M, kTileRows, b / g.nt, l);
   else
-    t = {0, 0, (b / g.nt) << kTileShift, g.M};
+    t = {0, 0, (b / g.nt) * kTileRows, g.M};
   if (t.m0 >= t.end) return;
   const int n0 = int(b % g.nt) * TN, K = g.K, N = g.N;
   uint16_t *y = g.y;
@@ -1535,7 +1566,7 @@ void launch_product(ProductArgs g, hipStream_t s) {
       return;
     }
   }
-  g.mt = tile_bound(g.M, g.G, kTileShift);
+  g.mt = tile_bound(g.M, g.G, kTileRows);
   if constexpr (sizeof(T) == 2 && !WT) {
     // 256 columns at a time, so that a row's SiLU is computed half as often: against
     // 128, K = 512, N = 512, 1 and 100 types: M = 32,000 38 against 29 and 50 against
@@ -1579,51 +1610,77 @@ void launch_product(ProductArgs g, hipStream_t s) {
   }
 }
 
+// Of dW's sums: tiles, rows of a range, slots of partial sums.
+//
+// As many workgroups as stay on the chip together (`all`), or a few times as many, and
+// not one more, since a few left over would take as long again: with n = G tiles
+// workgroups, ranges of R rows are at most M tiles / R + n of them.  Ranges end at about
+// 4096 rows, since groups differ in length and a partial sum's 2 x 64 KB no longer count.
+// Where the groups alone are about as many workgroups, ranges only even out their
+// lengths.  fp32 against ranges of a power of two, 2/3 to 4/3 of 768 workgroups, us: M =
+// 523,599 K = 128 N = 64 of 16 types 146 against 116, M = 300,000 192 x 128 257 against
+// 178, M = 1,000,000 256 x 100 574 against 570, and 935 with ranges 2% too short.
 struct WeightShape {
-  int shift, kt, nt;
+  int range, kt, nt;
+  bool wide, few;
   int64_t slot, slots;
 };
-WeightShape weight_shape(int64_t M, int K, int N) {
+WeightShape weight_shape(int dtype, int64_t M, int K, int N, int G) {
   WeightShape z;
   z.kt = int(K <= 64 ? 1 : cdiv(K, 128));
   z.nt = int(N <= 64 ? 1 : cdiv(N, 128));
-  // about 768 workgroups, ranges of at least 256 rows
-  const int64_t rows = M * z.kt * z.nt / 768;
-  z.shift = 8;
-  while (3 * (int64_t(1) << z.shift) < 2 * rows && z.shift < 30) ++z.shift;
+  z.wide = dtype == ALLEGRO_BF16 && K > 64 && N > 128 && M * z.kt * z.nt >= 131072;
+  if (z.wide) z.nt = int(cdiv(N, 256));
+  const int on_unit = z.wide || (dtype == ALLEGRO_F32 && K > 64 && N > 64) ? 2 : 3;
+  const int64_t tiles = int64_t(z.kt) * z.nt, n = G * tiles, all = 256 * on_unit;
+  constexpr int64_t most = 4096;
+  const int64_t rounds = std::max<int64_t>(1, cdiv(M * tiles / most + n, all));
+  const int64_t rows = n <= all / 2 ? cdiv(M * tiles, rounds * all - n) : std::min(cdiv(M * tiles, all), most);
+  z.range = int(cdiv(std::max<int64_t>(rows, 256), 64) * 64);
+  z.few = (M / z.range) * tiles + n <= 256;
   z.slot = cdiv(int64_t(K) * N, 4) * 4;
-  z.slots = M > (int64_t(1) << z.shift) ? 2 * (M >> z.shift) + 1 : 0;
+  z.slots = M > z.range ? 2 * (M / z.range) + 1 : 0;
   return z;
 }
 
 template <class T>
 void launch_weight(WeightArgs g, const WeightShape &z, hipStream_t s) {
-  g.shift = z.shift;
+  g.range = z.range;
   g.kt = z.kt;
   g.nt = z.nt;
   g.slot = z.slot;
-  g.ranges = tile_bound(g.M, g.G, z.shift);
-  const bool wide = sizeof(T) == 2 && g.K > 64 && g.N > 128 && g.M * g.kt * g.nt >= 131072;
-  if (wide) g.nt = int(cdiv(g.N, 256));
-  const dim3 grid(unsigned(g.ranges * g.kt * g.nt)), block(kThreads);
+  g.ranges = tile_bound(g.M, g.G, z.range);
+  const dim3 grid(unsigned(g.ranges * g.kt * g.nt));
   if constexpr (sizeof(T) == 2) {
     // 256 columns of dW at a time, us, 1 and 100 types: K = 128, N = 256 M = 32,000 23
     // against 25, 100,000 44 against 38 and 60 against 54; K = 512, N = 512 M = 2,000 20
     // against 23, 32,000 66 against 57, 400,000 584 against 445 and 497 against 484
-    if (wide) hipLaunchKernelGGL((weight_kernel<T, 128, 256>), grid, dim3(tile_threads(256)), 0, s, g);
+    if (z.wide) hipLaunchKernelGGL((weight_kernel<T, 128, 256, 1>), grid, dim3(tile_threads(256)), 0, s, g);
   }
-  if (!wide) {
-    if (g.K <= 64 && g.N <= 64)
-      hipLaunchKernelGGL((weight_kernel<T, 64, 64>), grid, block, 0, s, g);
-    else if (g.K <= 64)
-      hipLaunchKernelGGL((weight_kernel<T, 64, 128>), grid, block, 0, s, g);
-    else if (g.N <= 64)
-      hipLaunchKernelGGL((weight_kernel<T, 128, 64>), grid, block, 0, s, g);
+  if (!z.wide) {
+    const int shape = (g.K > 64) * 2 + (g.N > 64);
+    auto launch = [&](auto buffers) {
+      constexpr int BUFS = buffers();
+      const dim3 block(BUFS * kThreads);
+      if (shape == 0)
+        hipLaunchKernelGGL((weight_kernel<T, 64, 64, BUFS>), grid, block, 0, s, g);
+      else if (shape == 1)
+        hipLaunchKernelGGL((weight_kernel<T, 64, 128, BUFS>), grid, block, 0, s, g);
+      else if (shape == 2)
+        hipLaunchKernelGGL((weight_kernel<T, 128, 64, BUFS>), grid, block, 0, s, g);
+      else
+        hipLaunchKernelGGL((weight_kernel<T, 128, 128, BUFS>), grid, block, 0, s, g);
+    };
+    // two buffers up to a workgroup per compute unit, us: fp32 M = 3,700 K = 128 N = 64 of
+    // 16 types 23.5 against 19.1, M = 20,000 128 x 128 34 against 28, bf16 20 against 18;
+    // with two workgroups (M = 30,000 512 x 512 of 4 types) 136 against 160
+    if (z.few)
+      launch(std::integral_constant<int, 2>{});
     else
-      hipLaunchKernelGGL((weight_kernel<T, 128, 128>), grid, block, 0, s, g);
+      launch(std::integral_constant<int, 1>{});
   }
   if (z.slots) {
-    const unsigned several = unsigned(std::min<int64_t>(g.G, g.M >> z.shift));
+    const unsigned several = unsigned(std::min<int64_t>(g.G, g.M / z.range));
     const int64_t parts = cdiv(int64_t(g.K) * g.N, 256);
     if (parts * several < 4096)
       hipLaunchKernelGGL((weight_sum_kernel<T, true>), dim3(unsigned(parts), several), dim3(kSumThreads), 0, s, g);
@@ -1639,7 +1696,7 @@ int check_product(int dtype, int act, int64_t M, int K, int N, int G) {
   if (act != ALLEGRO_ACT_NONE && act != ALLEGRO_ACT_SILU) return fail(ALLEGRO_E_INVALID, "unknown act %d", act);
   if ((rc = check_m(M)) || (rc = check_width(K, "K")) || (rc = check_width(N, "N")) || (rc = check_g(G))) return rc;
   // one workgroup per 128 x 128 tile, at most 2^31 - 1 of them
-  if (cdiv(std::max(K, N), 64) * tile_bound(M, G, kTileShift) > kMaxRows)
+  if (cdiv(std::max(K, N), 64) * tile_bound(M, G, kTileRows) > kMaxRows)
     return fail(ALLEGRO_E_UNSUPPORTED, "M=%lld rows of %d columns are more tiles than one launch takes", (long long)M,
                 std::max(K, N));
   return ALLEGRO_OK;
@@ -1672,8 +1729,8 @@ int allegro_grouped_matmul_workspace(int64_t M, int K, int N, int G, size_t *byt
   int rc;
   if ((rc = check_product(ALLEGRO_F32, ALLEGRO_ACT_NONE, M, K, N, G))) return rc;
   if (!bytes) return fail(ALLEGRO_E_INVALID, "bytes is NULL");
-  const WeightShape z = weight_shape(M, K, N);
-  *bytes = size_t(z.slots) * size_t(z.slot) * sizeof(float);
+  const WeightShape a = weight_shape(ALLEGRO_F32, M, K, N, G), b = weight_shape(ALLEGRO_BF16, M, K, N, G);
+  *bytes = size_t(std::max(a.slots, b.slots)) * size_t(a.slot) * sizeof(float);
   return ALLEGRO_OK;
 }
 
@@ -1704,7 +1761,7 @@ int allegro_grouped_matmul_backward(int dtype, int act, int64_t M, int K, int N,
   if (dX && ((rc = check_ptr(W, "W", e)) || (rc = check_rows(dX, "dX", lddx, K, e)))) return rc;
   WeightShape z{};
   if (dW) {
-    z = weight_shape(M, K, N);
+    z = weight_shape(dtype, M, K, N, G);
     if ((rc = check_workspace(workspace, workspace_bytes, size_t(z.slots) * size_t(z.slot) * sizeof(float)))) return rc;
   }
   if (dX) {
@@ -1744,7 +1801,7 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
                         xs, static_cast<const uint8_t *>(W),
                         ws, static_cast<uint16_t *>(Y),
                         ldy, int(cdiv(N, N <= 64 ? 64 : 128)),
-                        tile_bound(M, G, kTileShift)};
+                        tile_bound(M, G, kTileRows)};
   hipStream_t s = static_cast<hipStream_t>(stream);
   // Rows past stationary weights, or tiles, us, 1 and 64 types (before the scales
   // and stores of the former were gathered): M = 8,000 K = 512 N = 512 13 against 10
