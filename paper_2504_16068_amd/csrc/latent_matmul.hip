@@ -1629,7 +1629,7 @@ WeightShape weight_shape(int dtype, int64_t M, int K, int N, int G) {
   WeightShape z;
   z.kt = int(K <= 64 ? 1 : cdiv(K, 128));
   z.nt = int(N <= 64 ? 1 : cdiv(N, 128));
-  z.wide = dtype == ALLEGRO_BF16 && K > 64 && N > 128 && M * z.kt * z.nt >= 131072;
+  z.wide = dtype == ALLEGRO_BF16 && K > 64 && N > 128 && M * z.kt * z.nt >= 1 << 20;
   if (z.wide) z.nt = int(cdiv(N, 256));
   const int on_unit = z.wide || (dtype == ALLEGRO_F32 && K > 64 && N > 64) ? 2 : 3;
   const int64_t tiles = int64_t(z.kt) * z.nt, n = G * tiles, all = 256 * on_unit;
@@ -1652,9 +1652,10 @@ void launch_weight(WeightArgs g, const WeightShape &z, hipStream_t s) {
   g.ranges = tile_bound(g.M, g.G, z.range);
   const dim3 grid(unsigned(g.ranges * g.kt * g.nt));
   if constexpr (sizeof(T) == 2) {
-    // 256 columns of dW at a time, us, 1 and 100 types: K = 128, N = 256 M = 32,000 23
-    // against 25, 100,000 44 against 38 and 60 against 54; K = 512, N = 512 M = 2,000 20
-    // against 23, 32,000 66 against 57, 400,000 584 against 445 and 497 against 484
+    // 256 columns of dW at a time against 128, us, 1 and 100 types: K = 128, N = 256
+    // M = 32,000 22.5 against 26.7 and 26 against 28, 100,000 39 against 39 and 43 against 44;
+    // K = 512, N = 512 M = 32,000 59 against 59 and 70 against 78, 400,000 476 against 403
+    // and 482 against 439; M = 100,003 1024 x 512 of 100 types 245 against 230
     if (z.wide) hipLaunchKernelGGL((weight_kernel<T, 128, 256, 1>), grid, dim3(tile_threads(256)), 0, s, g);
   }
   if (!z.wide) {
@@ -1803,11 +1804,13 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
                         ldy, int(cdiv(N, N <= 64 ? 64 : 128)),
                         tile_bound(M, G, kTileRows)};
   hipStream_t s = static_cast<hipStream_t>(stream);
-  // Rows past stationary weights, or tiles, us, 1 and 64 types (before the scales
-  // and stores of the former were gathered): M = 8,000 K = 512 N = 512 13 against 10
-  // and 24 against 14; M = 32,000 24 against 23 and 32 against 29; M = 128,000 56
-  // against 76 and 69 against 83; M = 128,000 K = 128 N = 64 15 against 11.
-  if (N > 64 && K >= 16 && K <= kStreamF8K && M >= 65536 && M >= 1024 * int64_t(G)) {
+  // Tiles against rows past stationary weights, us, 1 and 64 types: K = 512, N = 512 M =
+  // 32,000 23 against 28 and 28 against 29 (16 types), 64,000 41 against 39 and 48 against
+  // 48, 128,000 76 against 60 and 83 against 69; 1024 x 1024 M = 32,000 66 against 56,
+  // 128,000 295 against 191 and 309 against 225, and 349 against 321 with 225; 128,000 1024 x
+  // 128 39 against 41 and 48 against 44, 256 x 128 19 against 21.5 and 24 against 23.
+  const int64_t nt = cdiv(N, 128);
+  if (N > 64 && K >= 16 && K <= kStreamF8K && M * nt >= 131072 && M >= 1024 * int64_t(G)) {
     g.nt = int(cdiv(N, 128));
     g.mt = std::max(1, kStreamGroups / g.nt);
     hipLaunchKernelGGL(product_f8_stream_kernel, dim3(unsigned(g.mt * g.nt)), dim3(kStreamThreads), 0, s, g);

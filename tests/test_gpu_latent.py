@@ -180,6 +180,14 @@ def test_products_over_many_rows(at, dtype, m, k, n, g):
     _product_case(at, m, k, n, g, dtype, True)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n,g", [(9000, 300, 500, 4), (17003, 257, 390, 6), (66000, 513, 390, 3), (30000, 400, 256, 200)])
+def test_products_over_many_tiles(at, dtype, m, k, n, g):
+    """Grids from a tile to a compute unit up to many, whose tiles are of other widths."""
+    _note(f"[gpu] product M={m} K={k} N={n} G={g} {dtype} many tiles")
+    _product_case(at, m, k, n, g, dtype, True)
+
+
 @pytest.mark.parametrize("m,k,n,g,act", [(66003, 192, 128, 3, False), (70000, 128, 64, 100, True), (65600, 20, 130, 16, True),
                                          (65536, 65, 191, 5, False), (90001, 4, 3, 128, False), (65537, 384, 61, 2, True)])
 def test_products_of_many_rows(at, m, k, n, g, act):
@@ -518,6 +526,17 @@ def test_f8_products_strides_and_alignment(at, pad, shift):
     _note(f"[gpu] 8-bit product strides pad={pad} shift={shift}")
     _f8_case(at, 200, 272, 144, 3, pad, shift)
     _f8_case(at, 200, 128, 64, 3, pad, shift, rows=False)
+
+
+@pytest.mark.parametrize("m,k,n,g,typed,rows", [(70000, 130, 160, 3, True, True), (131075, 16, 66, 100, True, True),
+                                                (66001, 1152, 256, 2, True, False), (131072, 40, 128, 1, False, False),
+                                                (65600, 257, 391, 64, True, True)])
+def test_f8_products_of_many_rows(at, m, k, n, g, typed, rows):
+    """Rows that are streamed past stationary weights."""
+    _note(f"[gpu] 8-bit product M={m} K={k} N={n} G={g} streamed")
+    _f8_case(at, m, k, n, g, typed=typed, rows=rows)
+    if k == 130:
+        _f8_case(at, m, k, n, g, 3, 1)
 
 
 def test_f8_products_one_group(at):
