@@ -1640,14 +1640,14 @@ void launch_product(ProductArgs g, hipStream_t s) {
 
 // Of dW's sums: tiles, rows of a range, slots of partial sums.
 //
-// As many workgroups as stay on the chip together (`all`), or a few times as many, and
-// not one more, since a few left over would take as long again: with n = G tiles
-// workgroups, ranges of R rows are at most M tiles / R + n of them.  Ranges end at about
-// 4096 rows, since groups differ in length and a partial sum's 2 x 64 KB no longer count.
-// Where the groups alone are about as many workgroups, ranges only even out their
-// lengths.  fp32 against ranges of a power of two, 2/3 to 4/3 of 768 workgroups, us: M =
-// 523,599 K = 128 N = 64 of 16 types 146 against 116, M = 300,000 192 x 128 257 against
-// 178, M = 1,000,000 256 x 100 574 against 570, and 935 with ranges 2% too short.
+// As many workgroups as stay on the chip together (`all`) and not one more, since a few
+// left over would take as long again: with n = G tiles workgroups, ranges of R rows are at
+// most M tiles / R + n of them.  Where the groups' ends, half a range each, would leave a
+// sixteenth of the chip idle, twice as many; where the groups alone fill half of it, ranges only
+// even out their lengths.  No more than 2 `all` tiles of partial sums in any case.  fp32
+// against ranges of a power of two, 2/3 to 4/3 of 768 workgroups, us: M = 523,599 K = 128
+// N = 64 of 16 types 146 against 116, M = 300,000 192 x 128 257 against 178, M = 1,000,000
+// 256 x 100 574 against 570, and 935 with ranges 2% too short.
 struct WeightShape {
   int range, kt, nt;
   bool wide, few;
@@ -1661,10 +1661,8 @@ WeightShape weight_shape(int dtype, int64_t M, int K, int N, int G) {
   if (z.wide) z.nt = int(cdiv(N, 256));
   const int on_unit = z.wide || (dtype == ALLEGRO_F32 && K > 64 && N > 64) ? 2 : 3;
   const int64_t tiles = int64_t(z.kt) * z.nt, n = G * tiles, all = 256 * on_unit;
-  constexpr int64_t most = 4096;
-  const int64_t rounds = std::max<int64_t>(1, cdiv(M * tiles / most + n, all));
-  const int64_t rows = n <= all / 2 ? cdiv(M * tiles, rounds * all - n) : std::min(cdiv(M * tiles, all), most);
-  z.range = int(cdiv(std::max<int64_t>(rows, 256), 64) * 64);
+  const int64_t rows = cdiv(M * tiles, n <= all / 8 ? all - n : n <= all / 2 ? 2 * all - n : all);
+  z.range = int(cdiv(std::min<int64_t>(std::max<int64_t>(rows, 256), 1 << 30), 64) * 64);
   z.few = (M / z.range) * tiles + n <= 256;
   z.slot = cdiv(int64_t(K) * N, 4) * 4;
   z.slots = M > z.range ? 2 * (M / z.range) + 1 : 0;

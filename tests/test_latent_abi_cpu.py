@@ -62,6 +62,14 @@ def test_workspace_sizes():
         assert ex.value.code == ALLEGRO_E_INVALID
 
 
+@pytest.mark.parametrize("m,k,n,g", [(10 ** 7, 1024, 1024, 1), (10 ** 7, 1024, 1024, 16), (10 ** 6, 128, 64, 225),
+                                     (2 ** 31 - 1, 64, 64, 4), (2 ** 25, 65536, 256, 1)])
+def test_product_workspace_is_bounded(m, k, n, g):
+    """Partial sums of dw: a few for each tile on the chip, whatever the number of rows."""
+    tiles = -(-k // 128) * -(-n // 128)
+    assert latent.allegro_grouped_matmul_workspace(m, k, n, g) <= 4 * (2 * 1024 + tiles) * 128 * 128 * 4
+
+
 def test_group_rows_refuses():
     fn = latent.library().allegro_group_rows
     good = [5000, 4, OK, OK, OK, OK, 1 << 20, None]
