@@ -103,6 +103,12 @@ def test_group_rows(at, m, g):
     assert np.array_equal(offsets.cpu().numpy(), np.concatenate([[0], np.cumsum(counts)]))
 
 
+@pytest.mark.parametrize("m,g", [(131072, 255), (131073, 16), (9000, 256), (30000, 1000), (1048820, 225)])
+def test_group_rows_by_chunks(at, m, g):
+    """Few and many chunks of rows, types by the hundred."""
+    test_group_rows(at, m, g)
+
+
 def test_group_rows_without_rows_or_types(at):
     offsets, rows = at.allegro_group_rows(torch.empty(0, dtype=torch.int32, device=DEV), 5)
     assert offsets.tolist() == [0] * 6 and rows.numel() == 0
