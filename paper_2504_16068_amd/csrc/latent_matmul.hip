@@ -1016,9 +1016,7 @@ __global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 ? 4 :
     WeightArgs g) {
   constexpr int KS = Kind<T>::KS;
   constexpr bool F32 = sizeof(T) == 4;
-  // waves along the rows of dW; products of a wave
-  constexpr int NT = BUFS == 2 ? 512 : tile_threads(TN), WK = BUFS == 2 && TK > TN ? 4 : 2;
-  constexpr int MI = TK / 16 / WK, NI = TN / 16 / (NT / kWave / WK);
+  constexpr int NT = BUFS == 2 ? 512 : tile_threads(TN), MI = TK / 32, NI = TN / 16 / (NT / 128);
   using XTile = Across<T, TK, false, NT, tile_short(TN)>;
   using YTile = Across<T, TN, false, NT, tile_short(TN)>;
   __shared__ u32x4 x_lds[BUFS * XTile::SIZE], y_lds[BUFS * YTile::SIZE];
@@ -1068,7 +1066,7 @@ __global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 ? 4 :
   for (int i = 0; i < MI; ++i)
 #pragma unroll
     for (int j = 0; j < NI; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  const int wk = 16 * MI * (wave % WK), wn = 16 * NI * (wave / WK);
+  const int wk = 16 * MI * (wave % 2), wn = 16 * NI * (wave / 2);
   const typename XTile::Reader x_read(wk / 16, l);
   const typename YTile::Reader y_read(wn / 16, l);
   float sign = 1.f;
@@ -1663,7 +1661,18 @@ WeightShape weight_shape(int dtype, int64_t M, int K, int N, int G) {
   const int64_t tiles = int64_t(z.kt) * z.nt, n = G * tiles, all = 256 * on_unit;
   const int64_t rows = cdiv(M * tiles, n <= all / 8 ? all - n : n <= all / 2 ? 2 * all - n : all);
   z.range = int(cdiv(std::min<int64_t>(std::max<int64_t>(rows, 256), 1 << 30), 64) * 64);
+  // Up to a workgroup per compute unit: tiles of 64 x 64 instead, through two buffers, and
+  // while their ranges are few, shorter ones (from 1024 rows on, below which they would
+  // add the launch of their sums).  fp32, us, against 128 columns and two buffers: M =
+  // 1,640 192 x 103 25.6 against 17.5, and 14.7 with ranges of 128; 3,700 rows of 16 types
+  // 128 x 64 19.4, 16.1, 15.3; 20,000 128 x 128 28.6, 24.1 (22.5 with the ranges that are too
+  // many by the rule); 12,000 96 x 200 29.1, 24.3 (26.5); bf16 gains up to 3 us.
   z.few = (M / z.range) * tiles + n <= 256;
+  if (z.few) {
+    z.kt = int(cdiv(K, 64));
+    z.nt = int(cdiv(N, 64));
+    if (M >= 1024 && (M / 128) * z.kt * z.nt <= 256) z.range = 128;
+  }
   z.slot = cdiv(int64_t(K) * N, 4) * 4;
   z.slots = M > z.range ? 2 * (M / z.range) + 1 : 0;
   return z;
@@ -1685,26 +1694,16 @@ void launch_weight(WeightArgs g, const WeightShape &z, hipStream_t s) {
     if (z.wide) hipLaunchKernelGGL((weight_kernel<T, 128, 256, 1>), grid, dim3(tile_threads(256)), 0, s, g);
   }
   if (!z.wide) {
-    const int shape = (g.K > 64) * 2 + (g.N > 64);
-    auto launch = [&](auto buffers) {
-      constexpr int BUFS = buffers();
-      const dim3 block(BUFS * kThreads);
-      if (shape == 0)
-        hipLaunchKernelGGL((weight_kernel<T, 64, 64, BUFS>), grid, block, 0, s, g);
-      else if (shape == 1)
-        hipLaunchKernelGGL((weight_kernel<T, 64, 128, BUFS>), grid, block, 0, s, g);
-      else if (shape == 2)
-        hipLaunchKernelGGL((weight_kernel<T, 128, 64, BUFS>), grid, block, 0, s, g);
-      else
-        hipLaunchKernelGGL((weight_kernel<T, 128, 128, BUFS>), grid, block, 0, s, g);
-    };
-    // two buffers up to a workgroup per compute unit, us: fp32 M = 3,700 K = 128 N = 64 of
-    // 16 types 23.5 against 19.1, M = 20,000 128 x 128 34 against 28, bf16 20 against 18;
-    // with two workgroups (M = 30,000 512 x 512 of 4 types) 136 against 160
     if (z.few)
-      launch(std::integral_constant<int, 2>{});
+      hipLaunchKernelGGL((weight_kernel<T, 64, 64, 2>), grid, dim3(2 * kThreads), 0, s, g);
+    else if (g.K <= 64 && g.N <= 64)
+      hipLaunchKernelGGL((weight_kernel<T, 64, 64, 1>), grid, dim3(kThreads), 0, s, g);
+    else if (g.K <= 64)
+      hipLaunchKernelGGL((weight_kernel<T, 64, 128, 1>), grid, dim3(kThreads), 0, s, g);
+    else if (g.N <= 64)
+      hipLaunchKernelGGL((weight_kernel<T, 128, 64, 1>), grid, dim3(kThreads), 0, s, g);
     else
-      launch(std::integral_constant<int, 1>{});
+      hipLaunchKernelGGL((weight_kernel<T, 128, 128, 1>), grid, dim3(kThreads), 0, s, g);
   }
   if (z.slots) {
     const unsigned several = unsigned(std::min<int64_t>(g.G, g.M / z.range));
