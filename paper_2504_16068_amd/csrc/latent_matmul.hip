@@ -1216,7 +1216,7 @@ __global__ void fill_zero_kernel(int64_t n, T *p) {
 struct ProductF8Args {
   int64_t M;
   int K, N, G;
-  const int64_t *offsets;  // null: one group of all rows
+  const int64_t *offsets;  // null, and then rows too: one group of all rows
   const int32_t *rows;
   const uint8_t *x;  // [M][K]
   int64_t ldx;
@@ -1272,7 +1272,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
   if (t.m0 >= t.end) return;
   const int n0 = int(b % g.nt) * TN, K = g.K, N = g.N;
   uint16_t *y = g.y;
-  list_rows(srow, g.offsets ? g.rows : nullptr, t, g.M, tid);
+  list_rows(srow, g.rows, t, g.M, tid);
   __syncthreads();
   if (t.g == g.G) {
     zero_rows(srow, y, g.ldy, n0, N - n0 < TN ? N - n0 : TN, tid);
@@ -1820,6 +1820,7 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
       (rc = check_rows(X, "X", ldx, K, 1)) || (rc = check_ptr(xs, "xs", 4)) || (rc = check_ptr(W, "W", 1)) ||
       (rc = check_ptr(ws, "ws", 4)) || (rc = check_rows(Y, "Y", ldy, N, 2)))
     return rc;
+  if (!offsets) rows = nullptr;  // one group, of all rows in their own order
   ProductF8Args g{M,  K,
                         N,  G,
                         offsets, rows,
