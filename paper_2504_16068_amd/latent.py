@@ -6,6 +6,10 @@ Functions have the names of the C entry points; like those of the tensor product
 dtypes and devices, allocate with PyTorch what the caller does not pass, and hand raw pointers and
 the current HIP stream to the library.  Tensors of rows may be views with a row stride.  There is no
 fallback: without the compiled library importing this module raises.
+
+A call with `stream` (a torch.cuda.Stream) is one under `with torch.cuda.stream(stream)`: results and
+workspaces that it allocates belong to that stream.  Tensors of other streams are the caller's to order
+(wait_stream) and to keep until the call has run (record_stream).
 """
 
 from __future__ import annotations
@@ -149,12 +153,22 @@ def _groups(offsets, rows, g, m, index):
             0 if rows is None else _whole(rows, "rows", (m,), _I32, index))
 
 
-def _scratch(t, need, index):
+def _empty(shape, dtype, index, stream):
+    """Memory for a call on `stream` (None: the current one), allocated on that stream: the caching allocator hands
+    memory on in the order of the stream that it was allocated on, so only there does the next owner come after the
+    call."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
+
+
+def _scratch(t, need, index, stream):
     """(tensor that keeps it, address, bytes) of a workspace."""
     if need == 0:
         return None, 0, 0
     if t is None:
-        t = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
+        t = _empty((need,), torch.uint8, index, stream)
         return t, t.data_ptr(), need
     if not isinstance(t, _Tensor) or t.get_device() != index or not t.is_contiguous():
         raise ValueError(f"workspace must be a contiguous tensor on cuda:{index}")
@@ -190,12 +204,12 @@ def allegro_group_rows(types, n_groups: int, offsets=None, rows=None, workspace=
         raise ValueError(f"types must live on a GPU, not on {types.device}")
     need = allegro_group_rows_workspace(m, g)
     if offsets is None:
-        offsets = torch.empty(g + 1, dtype=_I64, device=types.device)
+        offsets = _empty((g + 1,), _I64, index, stream)
     if rows is None:
-        rows = torch.empty(m, dtype=_I32, device=types.device)
+        rows = _empty((m,), _I32, index, stream)
     t_p = _whole(types, "types", (m,), _I32, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
-    keep, ws, ws_bytes = _scratch(workspace, need, index)
+    keep, ws, ws_bytes = _scratch(workspace, need, index, stream)
     _check(_lib.allegro_group_rows(m, g, t_p, o_p, r_p, ws, ws_bytes, _stream_of(stream, index)))
     return offsets, rows
 
@@ -209,7 +223,7 @@ def allegro_grouped_matmul(x, w, offsets, rows=None, act: int = ALLEGRO_ACT_NONE
     dt, shape = x.dtype, x.shape
     m, k = shape
     if out is None:
-        out = torch.empty((m, n), dtype=dt, device=x.device)
+        out = _empty((m, n), dt, index, stream)
     w_p = _whole(w, "w", (g, k, n), dt, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
     ldx, ldy = _rows(x, "x", shape, dt, index), _rows(out, "out", (m, n), dt, index)
@@ -236,13 +250,13 @@ def allegro_grouped_matmul_backward(x, w, dy, offsets, rows=None, act: int = ALL
     dx_p, lddx, dw_p, keep, ws, ws_bytes = 0, k, 0, None, 0, 0
     if need_dx:
         if dx is None:
-            dx = torch.empty((m, k), dtype=dt, device=x.device)
+            dx = _empty((m, k), dt, index, stream)
         dx_p, lddx = dx.data_ptr(), _rows(dx, "dx", shape, dt, index)
     if need_dw:
         if dw is None:
-            dw = torch.empty((g, k, n), dtype=dt, device=x.device)
+            dw = _empty((g, k, n), dt, index, stream)
         dw_p = _whole(dw, "dw", (g, k, n), dt, index)
-        keep, ws, ws_bytes = _scratch(workspace, allegro_grouped_matmul_workspace(m, k, n, g), index)
+        keep, ws, ws_bytes = _scratch(workspace, allegro_grouped_matmul_workspace(m, k, n, g), index, stream)
     _check(_lib.allegro_grouped_matmul_backward(code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, w_p, dy.data_ptr(),
                                                 lddy, dx_p, lddx, dw_p, ws, ws_bytes, _stream_of(stream, index)))
     return dx if need_dx else None, dw if need_dw else None
@@ -258,7 +272,7 @@ def allegro_grouped_matmul_fp8(x, x_scale, w, w_scale, offsets=None, rows=None, 
     g, n, _ = _weights(w, "N, K")
     kb, nb = (k + SCALE_BLOCK - 1) // SCALE_BLOCK, (n + SCALE_BLOCK - 1) // SCALE_BLOCK
     if out is None:
-        out = torch.empty((m, n), dtype=_BF16, device=x.device)
+        out = _empty((m, n), _BF16, index, stream)
     w_p = _whole(w, "w", (g, n, k), _F8, index)
     xs_p = _whole(x_scale, "x_scale", (m, kb), _F32, index)
     ws_p = _whole(w_scale, "w_scale", (g, nb, kb), _F32, index)
@@ -271,7 +285,7 @@ def allegro_grouped_matmul_fp8(x, x_scale, w, w_scale, offsets=None, rows=None, 
 
 # -------------------------------------------------------------------- norm
 
-def _norm_inputs(x, w, residual, total):
+def _norm_inputs(x, w, residual, total, stream):
     """(dtype code, device index, addresses and strides of x, residual, w and total, total)."""
     code, index = _matrix(x, "x")
     dt, shape = x.dtype, x.shape
@@ -280,7 +294,7 @@ def _norm_inputs(x, w, residual, total):
     if residual is not None:
         ldr, r_p = _rows(residual, "residual", shape, dt, index), residual.data_ptr()
         if total is None:
-            total = torch.empty(shape, dtype=dt, device=x.device)
+            total = _empty(shape, dt, index, stream)
     if total is not None:
         ldt, t_p = _rows(total, "total", shape, dt, index), total.data_ptr()
     return code, index, (x.data_ptr(), ldx, r_p, ldr, w_p, t_p, ldt), total
@@ -289,13 +303,13 @@ def _norm_inputs(x, w, residual, total):
 def allegro_rms_norm_forward(x, w, residual=None, eps: float = 1e-6, total=None, out=None, rstd=None, stream=None):
     """Returns (y [M, C], total [M, C], rstd [M]): total = x + residual (x itself without a residual), y = total *
     rstd * w with rstd = 1 / sqrt(mean(total^2) + eps).  total and rstd are what the backward takes."""
-    code, index, args, total = _norm_inputs(x, w, residual, total)
+    code, index, args, total = _norm_inputs(x, w, residual, total, stream)
     shape, dt = x.shape, x.dtype
     m, c = shape
     if out is None:
-        out = torch.empty(shape, dtype=dt, device=x.device)
+        out = _empty(shape, dt, index, stream)
     if rstd is None:
-        rstd = torch.empty(m, dtype=_F32, device=x.device)
+        rstd = _empty((m,), _F32, index, stream)
     rstd_p, ldy = _whole(rstd, "rstd", (m,), _F32, index), _rows(out, "out", shape, dt, index)
     _check(_lib.allegro_rms_norm_forward(code, m, c, eps, *args, out.data_ptr(), ldy, rstd_p,
                                          _stream_of(stream, index)))
@@ -304,14 +318,14 @@ def allegro_rms_norm_forward(x, w, residual=None, eps: float = 1e-6, total=None,
 
 def allegro_rms_norm_fp8(x, w, residual=None, eps: float = 1e-6, total=None, q=None, scale=None, stream=None):
     """Returns (q [M, C] float8_e4m3fn, scale [M, ceil(C/128)], total [M, C]): the norm as q * scale."""
-    code, index, args, total = _norm_inputs(x, w, residual, total)
+    code, index, args, total = _norm_inputs(x, w, residual, total, stream)
     shape = x.shape
     m, c = shape
     blocks = (c + SCALE_BLOCK - 1) // SCALE_BLOCK
     if q is None:
-        q = torch.empty(shape, dtype=_F8, device=x.device)
+        q = _empty(shape, _F8, index, stream)
     if scale is None:
-        scale = torch.empty((m, blocks), dtype=_F32, device=x.device)
+        scale = _empty((m, blocks), _F32, index, stream)
     scale_p, ldq = _whole(scale, "scale", (m, blocks), _F32, index), _rows(q, "q", shape, _F8, index)
     _check(_lib.allegro_rms_norm_fp8(code, m, c, eps, *args, q.data_ptr(), ldq, scale_p, _stream_of(stream, index)))
     return q, scale, x if total is None else total
@@ -334,11 +348,11 @@ def allegro_rms_norm_backward(total, w, rstd, dy, dtotal=None, dx=None, dw=None,
     if dtotal is not None:
         ldds, ds_p = _rows(dtotal, "dtotal", shape, dt, index), dtotal.data_ptr()
     if dx is None:
-        dx = torch.empty(shape, dtype=dt, device=total.device)
+        dx = _empty(shape, dt, index, stream)
     if dw is None:
-        dw = torch.empty(c, dtype=_F32, device=total.device)
+        dw = _empty((c,), _F32, index, stream)
     dw_p, lddx = _whole(dw, "dw", (c,), _F32, index), _rows(dx, "dx", shape, dt, index)
-    keep, ws, ws_bytes = _scratch(workspace, allegro_rms_norm_workspace(m, c), index)
+    keep, ws, ws_bytes = _scratch(workspace, allegro_rms_norm_workspace(m, c), index, stream)
     _check(_lib.allegro_rms_norm_backward(code, m, c, total.data_ptr(), ldt, w_p, rstd_p, dy.data_ptr(), lddy, ds_p, ldds,
                                           dx.data_ptr(), lddx, dw_p, ws, ws_bytes, _stream_of(stream, index)))
     return dx, dw
