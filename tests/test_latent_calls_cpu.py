@@ -23,8 +23,8 @@ class _OnGpu(torch.Tensor):
 class _Lib:
     """The library with recorded launches; its host arithmetic is called."""
 
-    def __init__(self, lib, launches):
-        self.lib, self.launches = lib, launches
+    def __init__(self, lib, launches, devices, device):
+        self.lib, self.launches, self.devices, self.device = lib, launches, devices, device
 
     def __getattr__(self, name):
         if name.endswith("_workspace"):
@@ -32,14 +32,15 @@ class _Lib:
 
         def launch(*args):
             self.launches.append((name, args[-1]))
+            self.devices.append(self.device())
             return 0
         return launch
 
 
 @pytest.fixture
 def calls(monkeypatch):
-    """Records: launches (name, stream handle), allocations (bytes, stream or None)."""
-    rec = SimpleNamespace(launches=[], allocated=[], stream=None)
+    """Records: launches (name, stream handle) and the devices current at them, allocations (bytes, stream or None)."""
+    rec = SimpleNamespace(launches=[], devices=[], allocated=[], stream=None, device=0)
 
     def empty(shape, dtype, device=None):
         t = torch.empty(shape, dtype=dtype)
@@ -52,11 +53,18 @@ def calls(monkeypatch):
         yield
         rec.stream = before
 
-    cuda = SimpleNamespace(stream=stream, current_device=lambda: 0)
+    @contextlib.contextmanager
+    def device(index):
+        before, rec.device = rec.device, index
+        yield
+        rec.device = before
+
+    cuda = SimpleNamespace(stream=stream, device=device, current_device=lambda: rec.device)
     monkeypatch.setattr(latent, "torch", SimpleNamespace(empty=empty, cuda=cuda, Tensor=torch.Tensor, uint8=torch.uint8,
                                                          device=lambda *a: a))
     monkeypatch.setattr(latent, "_raw_stream", lambda index: CURRENT)
-    monkeypatch.setattr(latent, "_lib", _Lib(latent.library(), rec.launches))
+    monkeypatch.setattr(latent, "_current_device", lambda: rec.device, raising=False)
+    monkeypatch.setattr(latent, "_lib", _Lib(latent.library(), rec.launches, rec.devices, lambda: rec.device))
     return rec
 
 
@@ -96,7 +104,7 @@ def test_what_a_call_allocates_belongs_to_its_stream(calls, i):
     another stream than the current one are allocated on that stream, or the current stream's next tensor could
     take a workspace that the call still uses."""
     name, call, outputs, workspace = _entries()[i]
-    side = SimpleNamespace(cuda_stream=SIDE)
+    side = SimpleNamespace(cuda_stream=SIDE, device=torch.device("cuda", 0))
     call(stream=side)
     assert calls.launches == [(name, SIDE)]
     assert sum(n for n, _ in calls.allocated) == outputs + workspace
@@ -106,3 +114,16 @@ def test_what_a_call_allocates_belongs_to_its_stream(calls, i):
     call()
     assert calls.launches == [(name, CURRENT)]
     assert all(s is None for _, s in calls.allocated)
+
+
+@pytest.mark.parametrize("i", range(7))
+def test_calls_run_on_their_tensors_device(calls, i):
+    """The tensors' device is made current for the launch, and a stream of another device is refused."""
+    name, call, _, _ = _entries()[i]
+    calls.device = 1
+    call()
+    assert calls.launches == [(name, CURRENT)] and calls.devices == [0] and calls.device == 1
+    other = SimpleNamespace(cuda_stream=SIDE, device=torch.device("cuda", 1))
+    with pytest.raises(ValueError, match="stream is one of cuda:1"):
+        call(stream=other)
+    assert len(calls.launches) == 1
