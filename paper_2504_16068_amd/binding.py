@@ -6,6 +6,11 @@ allocates outputs with PyTorch when the caller passes none, and hands raw
 device pointers plus the current HIP stream to the library.  No arithmetic of
 the operation happens in Python, and there is no fallback: if the compiled
 library is missing, importing this module raises.
+
+A call with `stream` (a torch.cuda.Stream) is one under `with torch.cuda.stream(stream)`:
+outputs and workspaces that it allocates belong to that stream.  Tensors of other
+streams are the caller's to order (wait_stream) and to keep until the call has run
+(record_stream).
 """
 
 from __future__ import annotations
@@ -169,6 +174,20 @@ def _need(t, name, shape, dtype, device):
         raise ValueError(f"{name} must be contiguous")
 
 
+def _empty(shape, dtype, index, stream):
+    """Memory for a call on `stream` (None: the current one) of device `index`, allocated on that stream: the caching
+    allocator hands memory on in the order of the stream that it was allocated on, so only there does the next owner
+    come after the call."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
+
+
+def _like(stream, *tensors):
+    return tuple(_empty(t.shape, t.dtype, t.device.index, stream) for t in tensors)
+
+
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
@@ -193,7 +212,7 @@ def allegro_env_embed(plan: Plan, row_ptr, w, Y, env=None, stream=None):
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
     if env is None:
-        env = torch.empty((n, plan.U, plan.d2), device=dev, dtype=torch.float32)
+        env = _empty((n, plan.U, plan.d2), torch.float32, dev.index, stream)
     _need(env, "env", (n, plan.U, plan.d2), torch.float32, dev)
     _check(_lib.allegro_env_embed(plan.handle, n, e, _ptr(row_ptr), _ptr(w), _ptr(Y), _ptr(env),
                                   _stream(stream, dev)))
@@ -207,7 +226,7 @@ def allegro_tp_forward(plan: Plan, row_ptr, x, env, path_w, out=None, stream=Non
     _need(env, "env", (n, plan.U, plan.d2), torch.float32, dev)
     _need(path_w, "path_w", (plan.n_paths, plan.U), torch.float32, dev)
     if out is None:
-        out = torch.empty_like(x)
+        out, = _like(stream, x)
     _need(out, "out", (e, plan.U, plan.d1), torch.float32, dev)
     _check(_lib.allegro_tp_forward(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w), _ptr(out),
                                    _stream(stream, dev)))
@@ -225,7 +244,7 @@ def allegro_tp_backward(plan: Plan, row_ptr, x, env, path_w, grad_out, w, Y, out
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
     if outs is None:
-        outs = (torch.empty_like(x), torch.empty_like(env), torch.empty_like(w), torch.empty_like(Y))
+        outs = _like(stream, x, env, w, Y)
     gx, genv, gw, gy = outs
     _need(gx, "grad_x", (e, plan.U, plan.d1), torch.float32, dev)
     _need(genv, "grad_env", (n, plan.U, plan.d2), torch.float32, dev)
@@ -256,8 +275,7 @@ def allegro_tp_backward_train(plan: Plan, row_ptr, x, env, path_w, grad_out, w, 
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
     if outs is None:
-        outs = (torch.empty_like(x), torch.empty_like(env), torch.empty_like(w), torch.empty_like(Y),
-                torch.empty_like(path_w))
+        outs = _like(stream, x, env, w, Y, path_w)
     gx, genv, gw, gy, gpw = outs
     _need(gx, "grad_x", (e, plan.U, plan.d1), torch.float32, dev)
     _need(genv, "grad_env", (n, plan.U, plan.d2), torch.float32, dev)
@@ -266,7 +284,7 @@ def allegro_tp_backward_train(plan: Plan, row_ptr, x, env, path_w, grad_out, w, 
     _need(gpw, "grad_path_w", (plan.n_paths, plan.U), torch.float32, dev)
     need = allegro_tp_backward_workspace(plan, n)
     if workspace is None:
-        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        workspace = _empty((max(need, 16),), torch.uint8, dev.index, stream)
     if workspace.device != torch.device(dev) or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the same device")
     _check(_lib.allegro_tp_backward_train(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w),
@@ -288,8 +306,7 @@ def allegro_tp_backward_train_noalloc(plan: Plan, row_ptr, x, env, path_w, grad_
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
     if outs is None:
-        outs = (torch.empty_like(x), torch.empty_like(env), torch.empty_like(w), torch.empty_like(Y),
-                torch.empty_like(path_w))
+        outs = _like(stream, x, env, w, Y, path_w)
     gx, genv, gw, gy, gpw = outs
     _need(gx, "grad_x", (e, plan.U, plan.d1), torch.float32, dev)
     _need(genv, "grad_env", (n, plan.U, plan.d2), torch.float32, dev)
@@ -308,7 +325,7 @@ def allegro_sh_forward(plan: Plan, vec, Y=None, stream=None):
     e = vec.shape[0]
     _need(vec, "vec", (e, 3), torch.float64, dev)
     if Y is None:
-        Y = torch.empty((e, plan.d2), device=dev, dtype=torch.float32)
+        Y = _empty((e, plan.d2), torch.float32, dev.index, stream)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
     _check(_lib.allegro_sh_forward(plan.handle, e, _ptr(vec), _ptr(Y), _stream(stream, dev)))
     return Y
@@ -321,7 +338,7 @@ def allegro_sh_backward(plan: Plan, vec, grad_Y, grad_vec=None, stream=None):
     _need(vec, "vec", (e, 3), torch.float64, dev)
     _need(grad_Y, "grad_Y", (e, plan.d2), torch.float32, dev)
     if grad_vec is None:
-        grad_vec = torch.empty((e, 3), device=dev, dtype=torch.float64)
+        grad_vec = _empty((e, 3), torch.float64, dev.index, stream)
     _need(grad_vec, "grad_vec", (e, 3), torch.float64, dev)
     _check(_lib.allegro_sh_backward(plan.handle, e, _ptr(vec), _ptr(grad_Y), _ptr(grad_vec), _stream(stream, dev)))
     return grad_vec
@@ -343,9 +360,9 @@ def allegro_layer_buffers(plan: Plan, L: int, H: int, n_centers: int, n_edges: i
     return sv.value, ws.value
 
 
-def _bytes_buffer(t, need, name, device):
+def _bytes_buffer(t, need, name, device, stream):
     if t is None:
-        return torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        return _empty((max(need, 16),), torch.uint8, device.index, stream)
     if t.device != torch.device(device) or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor on {device}")
     return t
@@ -371,11 +388,11 @@ def allegro_layer_forward(plan: Plan, L: int, H: int, row_ptr, h, V, Y, weights,
     """Returns (h_out, V_out, saved); weights maps A, W, Mix, B1, B2 to device tensors."""
     dev, n, e = _layer_inputs(plan, L, H, row_ptr, h, V, Y, weights)
     sv_need, _ = allegro_layer_buffers(plan, L, H, n, e)
-    h_out = torch.empty_like(h) if h_out is None else h_out
-    V_out = torch.empty_like(V) if V_out is None else V_out
+    h_out = _like(stream, h)[0] if h_out is None else h_out
+    V_out = _like(stream, V)[0] if V_out is None else V_out
     _need(h_out, "h_out", (e, L), torch.float32, dev)
     _need(V_out, "V_out", (e, plan.U, plan.d1), torch.float32, dev)
-    saved = _bytes_buffer(saved, sv_need, "saved", dev)
+    saved = _bytes_buffer(saved, sv_need, "saved", dev, stream)
     _check(_lib.allegro_layer_forward(plan.handle, int(L), int(H), n, e, _ptr(row_ptr), _ptr(h), _ptr(V), _ptr(Y),
                                       *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(h_out), _ptr(V_out),
                                       _ptr(saved), _nbytes(saved), _stream(stream, dev)))
@@ -390,14 +407,14 @@ def allegro_layer_backward(plan: Plan, L: int, H: int, row_ptr, h, V, Y, weights
     _need(dV_out, "dV_out", (e, plan.U, plan.d1), torch.float32, dev)
     _, ws_need = allegro_layer_buffers(plan, L, H, n, e)
     if outs is None:
-        outs = {"h": torch.empty_like(h), "V": torch.empty_like(V), "Y": torch.empty_like(Y)}
-        outs.update({k: torch.empty_like(weights[k]) for k in LAYER_WEIGHTS})
+        inputs = {"h": h, "V": V, "Y": Y, **{k: weights[k] for k in LAYER_WEIGHTS}}
+        outs = dict(zip(inputs, _like(stream, *inputs.values())))
     _need(outs["h"], "dh", (e, L), torch.float32, dev)
     _need(outs["V"], "dV", (e, plan.U, plan.d1), torch.float32, dev)
     _need(outs["Y"], "dY", (e, plan.d2), torch.float32, dev)
     for name, shape in layer_weight_shapes(plan, L, H).items():
         _need(outs[name], "d" + name, shape, torch.float32, dev)
-    workspace = _bytes_buffer(workspace, ws_need, "workspace", dev)
+    workspace = _bytes_buffer(workspace, ws_need, "workspace", dev, stream)
     _check(_lib.allegro_layer_backward(plan.handle, int(L), int(H), n, e, _ptr(row_ptr), _ptr(h), _ptr(V), _ptr(Y),
                                        *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(saved), _nbytes(saved),
                                        _ptr(dh_out), _ptr(dV_out), _ptr(outs["h"]), _ptr(outs["V"]), _ptr(outs["Y"]),

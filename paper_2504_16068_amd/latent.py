@@ -19,7 +19,7 @@ import os
 
 import torch
 
-from .binding import ALLEGRO_OK, AllegroError, _current_device, _raw_stream
+from .binding import ALLEGRO_OK, AllegroError, _current_device, _empty, _raw_stream
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liballegro_latent.so")
@@ -151,16 +151,6 @@ def _groups(offsets, rows, g, m, index):
     """Addresses of the grouping of m rows."""
     return (0 if offsets is None else _whole(offsets, "offsets", (g + 1,), _I64, index),
             0 if rows is None else _whole(rows, "rows", (m,), _I32, index))
-
-
-def _empty(shape, dtype, index, stream):
-    """Memory for a call on `stream` (None: the current one), allocated on that stream: the caching allocator hands
-    memory on in the order of the stream that it was allocated on, so only there does the next owner come after the
-    call."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", index))
 
 
 def _scratch(t, need, index, stream):
