@@ -192,12 +192,20 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream(stream, device):
-    if stream is None:
-        if _raw_stream is not None and device.index is not None:
-            return _raw_stream(device.index)
-        stream = torch.cuda.current_stream(device)
-    return stream.cuda_stream
+def _launch(fn, index, stream, *args):
+    """fn(*args, stream handle) for tensors of device `index`, which is the current one meanwhile: the handle
+    of a default stream names that of the current device."""
+    if stream is not None:
+        device = getattr(stream, "device", None)  # anything with a cuda_stream will do
+        if device is not None and device.index != index:
+            raise ValueError(f"stream is one of {device}, the tensors live on cuda:{index}")
+        handle = stream.cuda_stream
+    else:
+        handle = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
+    if _current_device() == index:
+        return fn(*args, handle)
+    with torch.cuda.device(index):
+        return fn(*args, handle)
 
 
 def _sizes(plan: Plan, row_ptr, n_edges):
@@ -214,8 +222,8 @@ def allegro_env_embed(plan: Plan, row_ptr, w, Y, env=None, stream=None):
     if env is None:
         env = _empty((n, plan.U, plan.d2), torch.float32, dev.index, stream)
     _need(env, "env", (n, plan.U, plan.d2), torch.float32, dev)
-    _check(_lib.allegro_env_embed(plan.handle, n, e, _ptr(row_ptr), _ptr(w), _ptr(Y), _ptr(env),
-                                  _stream(stream, dev)))
+    _check(_launch(_lib.allegro_env_embed, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(w), _ptr(Y),
+                   _ptr(env)))
     return env
 
 
@@ -228,8 +236,8 @@ def allegro_tp_forward(plan: Plan, row_ptr, x, env, path_w, out=None, stream=Non
     if out is None:
         out, = _like(stream, x)
     _need(out, "out", (e, plan.U, plan.d1), torch.float32, dev)
-    _check(_lib.allegro_tp_forward(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w), _ptr(out),
-                                   _stream(stream, dev)))
+    _check(_launch(_lib.allegro_tp_forward, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env),
+                   _ptr(path_w), _ptr(out)))
     return out
 
 
@@ -250,9 +258,8 @@ def allegro_tp_backward(plan: Plan, row_ptr, x, env, path_w, grad_out, w, Y, out
     _need(genv, "grad_env", (n, plan.U, plan.d2), torch.float32, dev)
     _need(gw, "grad_w", (e, plan.U), torch.float32, dev)
     _need(gy, "grad_Y", (e, plan.d2), torch.float32, dev)
-    _check(_lib.allegro_tp_backward(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w),
-                                    _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw), _ptr(gy),
-                                    _stream(stream, dev)))
+    _check(_launch(_lib.allegro_tp_backward, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env),
+                   _ptr(path_w), _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw), _ptr(gy)))
     return gx, genv, gw, gy
 
 
@@ -287,10 +294,9 @@ def allegro_tp_backward_train(plan: Plan, row_ptr, x, env, path_w, grad_out, w, 
         workspace = _empty((max(need, 16),), torch.uint8, dev.index, stream)
     if workspace.device != torch.device(dev) or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the same device")
-    _check(_lib.allegro_tp_backward_train(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w),
-                                          _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw),
-                                          _ptr(gy), _ptr(gpw), _ptr(workspace),
-                                          workspace.numel() * workspace.element_size(), _stream(stream, dev)))
+    _check(_launch(_lib.allegro_tp_backward_train, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(x),
+                   _ptr(env), _ptr(path_w), _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw),
+                   _ptr(gy), _ptr(gpw), _ptr(workspace), workspace.numel() * workspace.element_size()))
     return gx, genv, gw, gy, gpw
 
 
@@ -313,9 +319,9 @@ def allegro_tp_backward_train_noalloc(plan: Plan, row_ptr, x, env, path_w, grad_
     _need(gw, "grad_w", (e, plan.U), torch.float32, dev)
     _need(gy, "grad_Y", (e, plan.d2), torch.float32, dev)
     _need(gpw, "grad_path_w", (plan.n_paths, plan.U), torch.float32, dev)
-    _check(_lib.allegro_tp_backward_train_noalloc(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w),
-                                                  _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw),
-                                                  _ptr(gy), _ptr(gpw), _stream(stream, dev)))
+    _check(_launch(_lib.allegro_tp_backward_train_noalloc, dev.index, stream, plan.handle, n, e, _ptr(row_ptr),
+                   _ptr(x), _ptr(env), _ptr(path_w), _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw),
+                   _ptr(gy), _ptr(gpw)))
     return gx, genv, gw, gy, gpw
 
 
@@ -327,7 +333,7 @@ def allegro_sh_forward(plan: Plan, vec, Y=None, stream=None):
     if Y is None:
         Y = _empty((e, plan.d2), torch.float32, dev.index, stream)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
-    _check(_lib.allegro_sh_forward(plan.handle, e, _ptr(vec), _ptr(Y), _stream(stream, dev)))
+    _check(_launch(_lib.allegro_sh_forward, dev.index, stream, plan.handle, e, _ptr(vec), _ptr(Y)))
     return Y
 
 
@@ -340,7 +346,8 @@ def allegro_sh_backward(plan: Plan, vec, grad_Y, grad_vec=None, stream=None):
     if grad_vec is None:
         grad_vec = _empty((e, 3), torch.float64, dev.index, stream)
     _need(grad_vec, "grad_vec", (e, 3), torch.float64, dev)
-    _check(_lib.allegro_sh_backward(plan.handle, e, _ptr(vec), _ptr(grad_Y), _ptr(grad_vec), _stream(stream, dev)))
+    _check(_launch(_lib.allegro_sh_backward, dev.index, stream, plan.handle, e, _ptr(vec), _ptr(grad_Y),
+                   _ptr(grad_vec)))
     return grad_vec
 
 
@@ -393,9 +400,9 @@ def allegro_layer_forward(plan: Plan, L: int, H: int, row_ptr, h, V, Y, weights,
     _need(h_out, "h_out", (e, L), torch.float32, dev)
     _need(V_out, "V_out", (e, plan.U, plan.d1), torch.float32, dev)
     saved = _bytes_buffer(saved, sv_need, "saved", dev, stream)
-    _check(_lib.allegro_layer_forward(plan.handle, int(L), int(H), n, e, _ptr(row_ptr), _ptr(h), _ptr(V), _ptr(Y),
-                                      *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(h_out), _ptr(V_out),
-                                      _ptr(saved), _nbytes(saved), _stream(stream, dev)))
+    _check(_launch(_lib.allegro_layer_forward, dev.index, stream, plan.handle, int(L), int(H), n, e, _ptr(row_ptr),
+                   _ptr(h), _ptr(V), _ptr(Y), *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(h_out), _ptr(V_out),
+                   _ptr(saved), _nbytes(saved)))
     return h_out, V_out, saved
 
 
@@ -415,9 +422,8 @@ def allegro_layer_backward(plan: Plan, L: int, H: int, row_ptr, h, V, Y, weights
     for name, shape in layer_weight_shapes(plan, L, H).items():
         _need(outs[name], "d" + name, shape, torch.float32, dev)
     workspace = _bytes_buffer(workspace, ws_need, "workspace", dev, stream)
-    _check(_lib.allegro_layer_backward(plan.handle, int(L), int(H), n, e, _ptr(row_ptr), _ptr(h), _ptr(V), _ptr(Y),
-                                       *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(saved), _nbytes(saved),
-                                       _ptr(dh_out), _ptr(dV_out), _ptr(outs["h"]), _ptr(outs["V"]), _ptr(outs["Y"]),
-                                       *(_ptr(outs[k]) for k in LAYER_WEIGHTS), _ptr(workspace), _nbytes(workspace),
-                                       _stream(stream, dev)))
+    _check(_launch(_lib.allegro_layer_backward, dev.index, stream, plan.handle, int(L), int(H), n, e, _ptr(row_ptr),
+                   _ptr(h), _ptr(V), _ptr(Y), *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(saved), _nbytes(saved),
+                   _ptr(dh_out), _ptr(dV_out), _ptr(outs["h"]), _ptr(outs["V"]), _ptr(outs["Y"]),
+                   *(_ptr(outs[k]) for k in LAYER_WEIGHTS), _ptr(workspace), _nbytes(workspace)))
     return outs

@@ -19,7 +19,7 @@ import os
 
 import torch
 
-from .binding import ALLEGRO_OK, AllegroError, _current_device, _empty, _raw_stream
+from .binding import ALLEGRO_OK, AllegroError, _empty, _launch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liballegro_latent.so")
@@ -165,22 +165,6 @@ def _scratch(t, need, index, stream):
     return t, t.data_ptr(), t.numel() * t.element_size()
 
 
-def _launch(fn, index, stream, *args):
-    """Calls fn(*args, stream handle) for tensors of device `index`, which is the current one meanwhile: the handle
-    of a default stream names that of the current device."""
-    if stream is not None:
-        if stream.device.index != index:
-            raise ValueError(f"stream is one of {stream.device}, the tensors live on cuda:{index}")
-        handle = stream.cuda_stream
-    else:
-        handle = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
-    if _current_device() == index:
-        _check(fn(*args, handle))
-        return
-    with torch.cuda.device(index):
-        _check(fn(*args, handle))
-
-
 def _bytes(fn, *sizes):
     out = ctypes.c_size_t()
     _check(fn(*(int(v) for v in sizes), ctypes.byref(out)))
@@ -210,7 +194,7 @@ def allegro_group_rows(types, n_groups: int, offsets=None, rows=None, workspace=
     t_p = _whole(types, "types", (m,), _I32, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
     keep, ws, ws_bytes = _scratch(workspace, need, index, stream)
-    _launch(_lib.allegro_group_rows, index, stream, m, g, t_p, o_p, r_p, ws, ws_bytes)
+    _check(_launch(_lib.allegro_group_rows, index, stream, m, g, t_p, o_p, r_p, ws, ws_bytes))
     return offsets, rows
 
 
@@ -227,8 +211,8 @@ def allegro_grouped_matmul(x, w, offsets, rows=None, act: int = ALLEGRO_ACT_NONE
     w_p = _whole(w, "w", (g, k, n), dt, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
     ldx, ldy = _rows(x, "x", shape, dt, index), _rows(out, "out", (m, n), dt, index)
-    _launch(_lib.allegro_grouped_matmul, index, stream, code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, w_p,
-            out.data_ptr(), ldy)
+    _check(_launch(_lib.allegro_grouped_matmul, index, stream, code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx,
+                   w_p, out.data_ptr(), ldy))
     return out
 
 
@@ -257,8 +241,8 @@ def allegro_grouped_matmul_backward(x, w, dy, offsets, rows=None, act: int = ALL
             dw = _empty((g, k, n), dt, index, stream)
         dw_p = _whole(dw, "dw", (g, k, n), dt, index)
         keep, ws, ws_bytes = _scratch(workspace, allegro_grouped_matmul_workspace(m, k, n, g), index, stream)
-    _launch(_lib.allegro_grouped_matmul_backward, index, stream, code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx,
-            w_p, dy.data_ptr(), lddy, dx_p, lddx, dw_p, ws, ws_bytes)
+    _check(_launch(_lib.allegro_grouped_matmul_backward, index, stream, code, act, m, k, n, g, o_p, r_p, x.data_ptr(),
+                   ldx, w_p, dy.data_ptr(), lddy, dx_p, lddx, dw_p, ws, ws_bytes))
     return dx if need_dx else None, dw if need_dw else None
 
 
@@ -278,8 +262,8 @@ def allegro_grouped_matmul_fp8(x, x_scale, w, w_scale, offsets=None, rows=None, 
     ws_p = _whole(w_scale, "w_scale", (g, nb, kb), _F32, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
     ldx, ldy = _rows(x, "x", shape, _F8, index), _rows(out, "out", (m, n), _BF16, index)
-    _launch(_lib.allegro_grouped_matmul_fp8, index, stream, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, xs_p, w_p, ws_p,
-            out.data_ptr(), ldy)
+    _check(_launch(_lib.allegro_grouped_matmul_fp8, index, stream, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, xs_p, w_p,
+                   ws_p, out.data_ptr(), ldy))
     return out
 
 
@@ -311,7 +295,7 @@ def allegro_rms_norm_forward(x, w, residual=None, eps: float = 1e-6, total=None,
     if rstd is None:
         rstd = _empty((m,), _F32, index, stream)
     rstd_p, ldy = _whole(rstd, "rstd", (m,), _F32, index), _rows(out, "out", shape, dt, index)
-    _launch(_lib.allegro_rms_norm_forward, index, stream, code, m, c, eps, *args, out.data_ptr(), ldy, rstd_p)
+    _check(_launch(_lib.allegro_rms_norm_forward, index, stream, code, m, c, eps, *args, out.data_ptr(), ldy, rstd_p))
     return out, x if total is None else total, rstd
 
 
@@ -326,7 +310,7 @@ def allegro_rms_norm_fp8(x, w, residual=None, eps: float = 1e-6, total=None, q=N
     if scale is None:
         scale = _empty((m, blocks), _F32, index, stream)
     scale_p, ldq = _whole(scale, "scale", (m, blocks), _F32, index), _rows(q, "q", shape, _F8, index)
-    _launch(_lib.allegro_rms_norm_fp8, index, stream, code, m, c, eps, *args, q.data_ptr(), ldq, scale_p)
+    _check(_launch(_lib.allegro_rms_norm_fp8, index, stream, code, m, c, eps, *args, q.data_ptr(), ldq, scale_p))
     return q, scale, x if total is None else total
 
 
@@ -352,6 +336,6 @@ def allegro_rms_norm_backward(total, w, rstd, dy, dtotal=None, dx=None, dw=None,
         dw = _empty((c,), _F32, index, stream)
     dw_p, lddx = _whole(dw, "dw", (c,), _F32, index), _rows(dx, "dx", shape, dt, index)
     keep, ws, ws_bytes = _scratch(workspace, allegro_rms_norm_workspace(m, c), index, stream)
-    _launch(_lib.allegro_rms_norm_backward, index, stream, code, m, c, total.data_ptr(), ldt, w_p, rstd_p,
-            dy.data_ptr(), lddy, ds_p, ldds, dx.data_ptr(), lddx, dw_p, ws, ws_bytes)
+    _check(_launch(_lib.allegro_rms_norm_backward, index, stream, code, m, c, total.data_ptr(), ldt, w_p, rstd_p,
+                   dy.data_ptr(), lddy, ds_p, ldds, dx.data_ptr(), lddx, dw_p, ws, ws_bytes))
     return dx, dw

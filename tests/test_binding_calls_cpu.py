@@ -71,11 +71,10 @@ def calls(monkeypatch):
     monkeypatch.setattr(torch, "empty_like", empty_like)
     monkeypatch.setattr(torch.cuda, "stream", stream)
     monkeypatch.setattr(torch.cuda, "device", device)
+    monkeypatch.setattr(binding, "_raw_stream", lambda index: CURRENT)
+    monkeypatch.setattr(binding, "_current_device", lambda: rec.device)
     for module in (binding, latent):
-        lib = module.library()
-        monkeypatch.setattr(module, "_raw_stream", lambda index: CURRENT)
-        monkeypatch.setattr(module, "_current_device", lambda: rec.device)
-        monkeypatch.setattr(module, "_lib", _Lib(lib, rec))
+        monkeypatch.setattr(module, "_lib", _Lib(module.library(), rec))
     return rec
 
 
@@ -161,7 +160,7 @@ def test_what_a_call_allocates_belongs_to_its_stream(calls, entries, i):
     assert all(s is None for _, s in calls.allocated)
 
 
-@pytest.mark.parametrize("entries,i", ENTRIES[:7])
+@pytest.mark.parametrize("entries,i", ENTRIES)
 def test_calls_run_on_their_tensors_device(calls, entries, i):
     """The tensors' device is made current for the launch, and a stream of another device is refused."""
     name, call, _ = entries()[i]
