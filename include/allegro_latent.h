@@ -41,7 +41,11 @@
  *   value 448 ("e4m3fn").  Sums, norms and statistics are held in fp32 and
  *   rounded to dtype once, when an output is written; with ALLEGRO_BF16 the
  *   products round act(X) to bf16 as their operand when act is SiLU.  fp32
- *   products keep fp32 accuracy, 8-bit ones that of their bf16 output.
+ *   products keep fp32 accuracy, 8-bit ones that of their bf16 output.  With
+ *   ALLEGRO_F32 SiLU(a) is within (7 + |a| / 21) 2^-24 of its value and act'(a)
+ *   within (16 + |a| / 21) 2^-24 of its two terms' magnitudes (values below
+ *   2^-119 may become 0); with ALLEGRO_BF16 both are within 2^-17 before they
+ *   are rounded.
  *   Infinities and NaN propagate as in the formulas.
  *
  * Memory and ownership

@@ -45,15 +45,42 @@ constexpr int kTileRows = 128;  // rows of a tile
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 
-// SiLU and its derivative.  The hardware's exponential and reciprocal (1 ulp
-// each) leave about 2e-7 of the value; the library's correctly rounded division
-// costs ten more operations per element.
-__device__ __forceinline__ float sigmoid(float a) {
+// SiLU a sigma(a) and its derivative sigma(a) + a sigma(a) (1 - sigma(a)), from the
+// hardware's exponential and reciprocal (1 ulp each; the library's correctly
+// rounded division costs ten more operations per element).
+//
+// fp32: exp(-m) = 2^t exp(r) with t = -m log2(e), rounded, and r = -m - t ln 2 what the
+// rounding lost, at most 2^-17; exp(r) = 1 + r to 2^-35.  ln 2 itself is rounded, which
+// leaves m / 21 units of 2^-24.  With it SiLU is within (7 + |a| / 21) 2^-24 of its value,
+// the derivative within (16 + |a| / 21) 2^-24 of its terms' magnitudes.  m is limited so
+// that infinities leave r finite; of NaN a itself keeps one.  Measured, product and both
+// gradients of 523,599 rows, 128 x 64: 366 us, 359 without r, which is off by 60 units
+// at a = -80.
+constexpr float kLog2e = 0x1.715476p+0f, kLn2 = 0x1.62e43p-1f;
+__device__ __forceinline__ float silu(float a) {
+  const float m = __builtin_amdgcn_fmed3f(a, -128.0f, 128.0f);
+  const float t = -kLog2e * m, r = __builtin_fmaf(-kLn2, t, -m);
+  // exp(-a) is infinite below -88.7, hence the factor 1 + r above 0
+  return a * __builtin_amdgcn_rcpf(__builtin_fmaf(__builtin_amdgcn_exp2f(t), 1.0f + r, 1.0f));
+}
+// From e = exp(-|a|): sigma is 1 / (1 + e) or e / (1 + e) by the sign of a and 1 - sigma
+// the other one, so nothing is a difference.  e is zero for |a| above 87.3: what is lost
+// for negative a is below 2^-119.
+__device__ __forceinline__ float silu_grad(float a) {
+  const float m = fminf(fabsf(a), 128.0f);
+  const float t = -kLog2e * m, r = __builtin_fmaf(-kLn2, t, -m);
+  const float e0 = __builtin_amdgcn_exp2f(t), e = __builtin_fmaf(e0, r, e0);
+  const float d = __builtin_amdgcn_rcpf(1.0f + e), ed = e * d;
+  return __builtin_fmaf(a, ed * d, a < 0.0f ? ed : d);
+}
+// bf16 operands and results (half a unit is 2^-9) take the shorter form, off by up to
+// 2^-20 of the value at a = -20 and 2^-18 at -80: the exponent's rounding.
+__device__ __forceinline__ float sigmoid_bf16(float a) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-1.44269504088896341f * a));
 }
-__device__ __forceinline__ float silu(float a) { return a * sigmoid(a); }
-__device__ __forceinline__ float silu_grad(float a) {
-  const float s = sigmoid(a);
+__device__ __forceinline__ float silu_bf16(float a) { return a * sigmoid_bf16(a); }
+__device__ __forceinline__ float silu_grad_bf16(float a) {
+  const float s = sigmoid_bf16(a);
   return s * (1.0f + a * (1.0f - s));
 }
 
@@ -163,7 +190,8 @@ __device__ __forceinline__ u32x4 act_piece(u32x4 v, bool act) {  // of bf16 valu
   if (act) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
-      v[e] = bf16_pair(silu(__builtin_bit_cast(float, v[e] << 16)), silu(__builtin_bit_cast(float, v[e] & 0xffff0000u)));
+      v[e] = bf16_pair(silu_bf16(__builtin_bit_cast(float, v[e] << 16)),
+                       silu_bf16(__builtin_bit_cast(float, v[e] & 0xffff0000u)));
   }
   return v;
 }
@@ -701,7 +729,7 @@ __global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 && BU
       if (WT && pre) {
         const u32x4 p = load_bits<W>(pre + int64_t(r) * g.ldp + n, N - n);
 #pragma unroll
-        for (int e = 0; e < W; ++e) v[e] *= silu_grad(value_of<T>(p, e));
+        for (int e = 0; e < W; ++e) v[e] *= F32 ? silu_grad(value_of<T>(p, e)) : silu_grad_bf16(value_of<T>(p, e));
       }
       store_row<W>(y + int64_t(r) * g.ldy + n, v, N - n);
     }
