@@ -50,6 +50,10 @@ __device__ __forceinline__ float from_f32(float v) { return v; }
 template <>
 __device__ __forceinline__ uint16_t from_f32(float v) { return bf16_bits(v); }
 
+// Workgroups of a launch, which takes fewer than 2^32 threads.  Where there are more
+// tiles than this there are several launches; where a grid strides, it ends here.
+constexpr int64_t kMaxGrid = int64_t(1) << 22;
+
 inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 inline int after(const char *what) {

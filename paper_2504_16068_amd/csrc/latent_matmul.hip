@@ -569,6 +569,7 @@ struct ProductArgs {
   int act;     // SiLU on x (not transposed)
   int nt;      // column tiles
   int64_t mt;  // upper bound of the row tiles
+  int64_t first;  // the launch's first tile
 };
 
 // Threads of a tile TN columns wide: four waves, eight of a wide one.
@@ -606,7 +607,7 @@ __global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 && BU
   __shared__ u32x4 x_lds[BUFS * XTile::SIZE], w_lds[BUFS * WTile::SIZE];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
-  const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
+  const int64_t b = g.first + xcd_order(blockIdx.x, gridDim.x);
   const Tile t = find_tile(g.offsets, g.G, g.M, kTileRows, b / g.nt, l);
   if (t.m0 >= t.end) return;
   const int n0 = int(b % g.nt) * TN, K = g.K, N = g.N;
@@ -1255,6 +1256,7 @@ struct ProductF8Args {
   int64_t ldy;
   int nt;
   int64_t mt;
+  int64_t first;
 };
 
 // Drops the first `by` bytes of 16; zeros follow the last.
@@ -1291,7 +1293,7 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
   __shared__ u32x4 x_lds[kTileRows * KS / 16], w_lds[TN * KS / 16];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
-  const int64_t b = xcd_order(blockIdx.x, g.mt * g.nt);
+  const int64_t b = g.first + xcd_order(blockIdx.x, gridDim.x);
   Tile t;
   if (g.offsets)
     t = find_tile(g.offsets, g.G, g.M, kTileRows, b / g.nt, l);
@@ -1599,6 +1601,13 @@ __global__ __launch_bounds__(kStreamThreads, 2) void product_f8_stream_kernel(Pr
 }
 
 // ------------------------------------------------------------- launches
+// A workgroup for every tile, in as many launches as that takes.
+template <class Args>
+void launch_tiles(void (*kernel)(Args), Args g, int64_t tiles, int threads, hipStream_t s) {
+  for (g.first = 0; g.first < tiles; g.first += kMaxGrid)
+    hipLaunchKernelGGL(kernel, dim3(unsigned(std::min(tiles - g.first, kMaxGrid))), dim3(threads), 0, s, g);
+}
+
 template <class T, bool WT>
 void launch_product(ProductArgs g, hipStream_t s) {
   const bool narrow = g.N <= 64;
@@ -1632,11 +1641,10 @@ void launch_product(ProductArgs g, hipStream_t s) {
     const int64_t tiles = g.mt * nt;
     if (g.act && g.N > 128 && g.K >= 256 && tiles > 128) {
       g.nt = nt;
-      const dim3 grid{unsigned(tiles)}, block(2 * kThreads);
       if (tiles <= 256)
-        hipLaunchKernelGGL((product_kernel<T, 256, false, 2>), grid, block, 0, s, g);
+        launch_tiles(product_kernel<T, 256, false, 2>, g, tiles, 2 * kThreads, s);
       else
-        hipLaunchKernelGGL((product_kernel<T, 256, false, 1>), grid, block, 0, s, g);
+        launch_tiles(product_kernel<T, 256, false, 1>, g, tiles, 2 * kThreads, s);
       return;
     }
   }
@@ -1653,14 +1661,13 @@ void launch_product(ProductArgs g, hipStream_t s) {
   const int64_t tiles = g.mt * g.nt;
   if (narrow || tiles <= (!WT ? 320 : F32 ? 640 : 512) || 4 * g.N <= 3 * 128 * g.nt) {
     g.nt = int(cdiv(g.N, 64));
-    const dim3 grid{unsigned(g.mt * g.nt)};
-    if (F32 || grid.x <= 256) {
-      hipLaunchKernelGGL((product_kernel<T, 64, WT, 2>), grid, dim3(2 * kThreads), 0, s, g);
+    if (F32 || g.mt * g.nt <= 256) {
+      launch_tiles(product_kernel<T, 64, WT, 2>, g, g.mt * g.nt, 2 * kThreads, s);
       return;
     }
-    if constexpr (!F32) hipLaunchKernelGGL((product_kernel<T, 64, WT, 1>), grid, dim3(kThreads), 0, s, g);
+    if constexpr (!F32) launch_tiles(product_kernel<T, 64, WT, 1>, g, g.mt * g.nt, kThreads, s);
   } else {
-    hipLaunchKernelGGL((product_kernel<T, 128, WT, 1>), dim3(unsigned(tiles)), dim3(kThreads), 0, s, g);
+    launch_tiles(product_kernel<T, 128, WT, 1>, g, tiles, kThreads, s);
   }
 }
 
@@ -1749,9 +1756,9 @@ int check_product(int dtype, int act, int64_t M, int K, int N, int G) {
   if ((rc = check_dtype(dtype))) return rc;
   if (act != ALLEGRO_ACT_NONE && act != ALLEGRO_ACT_SILU) return fail(ALLEGRO_E_INVALID, "unknown act %d", act);
   if ((rc = check_m(M)) || (rc = check_width(K, "K")) || (rc = check_width(N, "N")) || (rc = check_g(G))) return rc;
-  // one workgroup per 128 x 128 tile, at most 2^31 - 1 of them
+  // one workgroup per tile of 128 rows and 64 columns or more, at most 2^31 - 1 of them
   if (cdiv(std::max(K, N), 64) * tile_bound(M, G, kTileRows) > kMaxRows)
-    return fail(ALLEGRO_E_UNSUPPORTED, "M=%lld rows of %d columns are more tiles than one launch takes", (long long)M,
+    return fail(ALLEGRO_E_UNSUPPORTED, "M=%lld rows of %d columns are more than 2^31 - 1 tiles", (long long)M,
                 std::max(K, N));
   return ALLEGRO_OK;
 }
@@ -1770,7 +1777,7 @@ int allegro_grouped_matmul(int dtype, int act, int64_t M, int K, int N, int G, c
   if ((rc = check_ptr(offsets, "offsets", 8)) || (rows && (rc = check_ptr(rows, "rows", 4))) ||
       (rc = check_rows(X, "X", ldx, K, e)) || (rc = check_ptr(W, "W", e)) || (rc = check_rows(Y, "Y", ldy, N, e)))
     return rc;
-  const ProductArgs g{M, K, N, G, offsets, rows, X, ldx, W, Y, ldy, nullptr, 0, act, 0, 0};
+  const ProductArgs g{M, K, N, G, offsets, rows, X, ldx, W, Y, ldy, nullptr, 0, act, 0, 0, 0};
   hipStream_t s = static_cast<hipStream_t>(stream);
   if (dtype == ALLEGRO_F32)
     launch_product<float, false>(g, s);
@@ -1820,7 +1827,7 @@ int allegro_grouped_matmul_backward(int dtype, int act, int64_t M, int K, int N,
   }
   if (dX) {
     // the same product with W transposed: the contraction runs along dY's columns
-    const ProductArgs g{M, N, K, G, offsets, rows, dY, lddy, W, dX, lddx, act ? X : nullptr, ldx, 0, 0, 0};
+    const ProductArgs g{M, N, K, G, offsets, rows, dY, lddy, W, dX, lddx, act ? X : nullptr, ldx, 0, 0, 0, 0};
     if (dtype == ALLEGRO_F32)
       launch_product<float, true>(g, s);
     else
@@ -1856,7 +1863,7 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
                         xs, static_cast<const uint8_t *>(W),
                         ws, static_cast<uint16_t *>(Y),
                         ldy, int(cdiv(N, N <= 64 ? 64 : 128)),
-                        tile_bound(M, G, kTileRows)};
+                        tile_bound(M, G, kTileRows), 0};
   hipStream_t s = static_cast<hipStream_t>(stream);
   // Tiles against rows past stationary weights, us, 1 and 64 types: K = 512, N = 512 M =
   // 32,000 23 against 28 and 28 against 29 (16 types), 64,000 41 against 39 and 48 against
@@ -1870,11 +1877,10 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
     hipLaunchKernelGGL(product_f8_stream_kernel, dim3(unsigned(g.mt * g.nt)), dim3(kStreamThreads), 0, s, g);
     return after("allegro_grouped_matmul_fp8");
   }
-  const dim3 grid(unsigned(g.mt * g.nt)), block(kThreads);
   if (N <= 64)
-    hipLaunchKernelGGL((product_f8_kernel<64>), grid, block, 0, s, g);
+    launch_tiles(product_f8_kernel<64>, g, g.mt * g.nt, kThreads, s);
   else
-    hipLaunchKernelGGL((product_f8_kernel<128>), grid, block, 0, s, g);
+    launch_tiles(product_f8_kernel<128>, g, g.mt * g.nt, kThreads, s);
   return after("allegro_grouped_matmul_fp8");
 }
 

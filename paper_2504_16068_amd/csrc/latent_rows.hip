@@ -829,7 +829,7 @@ void norm_forward(NormArgs g, hipStream_t s) {
         // (1.05M rows of 128 fp32: 766 us with the backward, 793 with 2048 persistent
         // workgroups); longer ones: as many workgroups as are resident, as each first
         // loads its columns' w
-        const unsigned grid = unsigned(std::min<int64_t>(cdiv(g.M, rows), nv() == 1 ? kMaxRows : 1024));
+        const unsigned grid = unsigned(std::min<int64_t>(cdiv(g.M, rows), nv() == 1 ? kMaxGrid : 1024));
         hipLaunchKernelGGL((norm_forward_kernel<T, vw(), nv(), F8>), dim3(grid), dim3(kThreads), 0, s, g);
       }))
     return;

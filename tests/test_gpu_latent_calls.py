@@ -113,3 +113,88 @@ def test_silu_over_its_range(at, m):
     dx, _ = at.allegro_grouped_matmul_backward(ends, one, torch.ones(6, 1, device=DEV), two, act=silu, need_dw=False)
     dx = dx[:, 0].cpu()
     assert dx[:3].isnan().all() and dx[3] == 0 and dx[4] == 1 and dx[5] == 0
+
+
+# -------------------------------------------------------------- largest sizes
+
+MOST = 2 ** 31 - 1  # rows
+
+
+def _needs(gib):
+    torch.cuda.empty_cache()
+    free = torch.cuda.mem_get_info()[0] / 2 ** 30
+    if free < gib:
+        pytest.skip(f"needs {gib} GiB of GPU memory, {free:.0f} are free")
+
+
+def _parts(m, part=2 ** 27):
+    return [slice(i, min(i + part, m)) for i in range(0, m, part)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16], ids=["f32", "bf16"])
+def test_products_of_the_most_rows(at, dtype):
+    """2^31 - 1 rows of one column are more tiles than a launch has workgroups for.  A product of one term is exact
+    in fp32 up to the parts that are left out (2^-24) and the roundings of six sums, and rounded once in bf16."""
+    _needs(40 if dtype is torch.float32 else 20)
+    _note(f"[gpu] product of 2^31 - 1 rows {dtype}")
+    base = torch.randn(2 ** 20, generator=_gen(1)).to(dtype).to(DEV)
+    x = torch.empty(MOST, 1, dtype=dtype, device=DEV)
+    for s in _parts(MOST, 2 ** 20):
+        x[s, 0] = base[:s.stop - s.start]
+    w = torch.tensor([1.25, -0.75], device=DEV).to(dtype).view(2, 1, 1)
+    cut, end = MOST // 3 + 5, MOST - 1001  # two groups, and rows of none
+    off = torch.tensor([0, cut, end], device=DEV)
+    y = torch.full((MOST, 1), 7.0, dtype=dtype, device=DEV)
+    at.allegro_grouped_matmul(x, w, off, out=y)
+    dx = torch.full((MOST, 1), 7.0, dtype=dtype, device=DEV) if dtype is BF16 else None
+    if dx is not None:
+        at.allegro_grouped_matmul_backward(x, w, x, off, dx=dx, need_dw=False)
+    for s in _parts(MOST):
+        r = torch.arange(s.start, s.stop, device=DEV)
+        factor = torch.where(r < cut, 1.25, torch.where(r < end, -0.75, 0.0))
+        want = x[s, 0].float() * factor
+        for got in (y,) if dx is None else (y, dx):
+            if dtype is BF16:
+                assert torch.equal(got[s, 0], want.to(BF16)), s
+            else:
+                assert bool(((got[s, 0] - want).abs() <= 8 * 2.0 ** -24 * want.abs()).all()), s
+    torch.cuda.empty_cache()
+
+
+def test_f8_products_of_the_most_rows(at):
+    """As above with 8-bit operands: one term of values that are powers of two is exact."""
+    _needs(40)
+    _note("[gpu] 8-bit product of 2^31 - 1 rows")
+    base = torch.exp2(torch.randint(-6, 8, (2 ** 20,), generator=_gen(2)).float()).to(F8).to(DEV)
+    x = torch.empty(MOST, 1, dtype=F8, device=DEV)
+    for s in _parts(MOST, 2 ** 20):
+        x[s, 0] = base[:s.stop - s.start]
+    xs = torch.full((MOST, 1), 0.5, device=DEV)
+    xs[MOST // 2:] = 0.25
+    w, ws = torch.full((1, 1, 1), 4.0, device=DEV).to(F8), torch.ones(1, 1, 1, device=DEV)
+    y = at.allegro_grouped_matmul_fp8(x, xs, w, ws, out=torch.full((MOST, 1), 7.0, dtype=BF16, device=DEV))
+    for s in _parts(MOST):
+        assert torch.equal(y[s, 0].float(), x[s, 0].float() * xs[s, 0] * 4.0), s
+    torch.cuda.empty_cache()
+
+
+def test_norm_of_many_long_rows(at):
+    """2^27 rows of 257 columns: more row groups than a launch has workgroups for.  Rows that repeat have the
+    results of a call on the first of them."""
+    _needs(150)
+    _note("[gpu] norm of 2^27 rows of 257 columns")
+    m, c, n = 2 ** 27, 257, 4096
+    base, w = _normal(_gen(3), n, c, dtype=BF16).to(DEV), torch.ones(c, device=DEV)
+    x = torch.empty(m, c, dtype=BF16, device=DEV)
+    x.view(m // n, n, c).copy_(base)
+    want, want_scale, _ = at.allegro_rms_norm_fp8(base, w)
+    q = torch.empty(m, c, dtype=F8, device=DEV)
+    q.view(torch.uint8).fill_(0x7F)
+    scale = torch.zeros(m, 3, device=DEV)
+    at.allegro_rms_norm_fp8(x, w, q=q, scale=scale)
+    del x
+    q = q.view(torch.uint8).view(m // n, n, c)
+    for s in _parts(m // n, 1024):
+        assert bool((q[s] == want.view(torch.uint8)).all()) and bool((scale.view(m // n, n, 3)[s] == want_scale).all()), s
+    del q, scale
+    torch.cuda.empty_cache()
