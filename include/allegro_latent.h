@@ -54,7 +54,8 @@
  *   width; W, dW, w, dw, rstd, scales, offsets and rows are contiguous.
  *   Pointers are aligned to their element; nothing more is asked of pointers,
  *   strides and widths, and all take the same kernels.  Outputs are overwritten
- *   and alias nothing.  Workspaces are 16-byte aligned and hold nothing between
+ *   and alias nothing, but that a norm's total may be its x or its residual
+ *   itself (the same pointer and row stride).  Workspaces are 16-byte aligned and hold nothing between
  *   calls; calls that share one must not overlap.  Nothing is allocated per call.
  *
  *   offsets and rows are read on the device: offsets out of order or range and

@@ -408,7 +408,7 @@ struct NormArgs {
 };
 
 // One pass: a row's sum of squares is formed across the lanes that hold it, then the
-// row is scaled, rounded and written from registers.  Bound by memory: 1,048,820 rows of
+// row is scaled, rounded and written from registers (so total may be x or residual).  Bound by memory: 1,048,820 rows of
 // 128 fp32 with residual and total 377 us (2.15 GB, 5.7 TB/s), 523,599 of 256 bf16 to 8
 // bits 178 us (0.95 GB, 5.3 TB/s), 20,001 of 1031 bf16 47 us (165 MB, 3.5 TB/s: rows of odd
 // width end within vectors, and 20,001 rows are five rounds of a workgroup).
@@ -542,7 +542,8 @@ __device__ __forceinline__ float block_sum(float v, float *tmp, int tid) {
 }
 
 // One workgroup per row, which it reads twice (the second time from the caches):
-// widths that registers do not hold.
+// widths that registers do not hold.  total is written in the second pass, by the
+// thread that reads the element for the last time: it may be x or residual itself.
 template <class T, bool F8>
 __global__ __launch_bounds__(kThreads) void norm_wide_forward_kernel(NormArgs g) {
   __shared__ float tmp[kWaves];
@@ -555,14 +556,16 @@ __global__ __launch_bounds__(kThreads) void norm_wide_forward_kernel(NormArgs g)
     for (int c = tid; c < C; c += kThreads) {
       const float s = to_f32(x[c]) + (res ? to_f32(res[c]) : 0.f);
       sq = __builtin_fmaf(s, s, sq);
-      if (total) total[c] = from_f32<T>(s);
     }
     const float rstd = 1.0f / sqrtf(block_sum(sq, tmp, tid) * (1.0f / float(C)) + g.eps);
     if (g.rstd && tid == 0) g.rstd[r] = rstd;
     if constexpr (!F8) {
       T *y = static_cast<T *>(g.y) + r * g.ldy;
-      for (int c = tid; c < C; c += kThreads)
-        y[c] = from_f32<T>((to_f32(x[c]) + (res ? to_f32(res[c]) : 0.f)) * rstd * g.w[c]);
+      for (int c = tid; c < C; c += kThreads) {
+        const float s = to_f32(x[c]) + (res ? to_f32(res[c]) : 0.f);
+        if (total) total[c] = from_f32<T>(s);
+        y[c] = from_f32<T>(s * rstd * g.w[c]);
+      }
     } else {
       uint8_t *q = static_cast<uint8_t *>(g.y) + r * g.ldy;
       const int blocks = (C + kBlock - 1) / kBlock, lane = tid % kWave;
@@ -571,7 +574,12 @@ __global__ __launch_bounds__(kThreads) void norm_wide_forward_kernel(NormArgs g)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int c = b * kBlock + i * kWave + lane;
-          y[i] = c < C ? (to_f32(x[c]) + (res ? to_f32(res[c]) : 0.f)) * rstd * g.w[c] : 0.f;
+          y[i] = 0.f;
+          if (c < C) {
+            const float s = to_f32(x[c]) + (res ? to_f32(res[c]) : 0.f);
+            if (total) total[c] = from_f32<T>(s);
+            y[i] = s * rstd * g.w[c];
+          }
         }
         const uint32_t m0 = abs_bits(y[0]), m1 = abs_bits(y[1]);
         const float sc = f8_scale(lanes_max(m0 > m1 ? m0 : m1, kWave)), inv = 1.0f / sc;

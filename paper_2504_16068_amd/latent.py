@@ -286,7 +286,8 @@ def _norm_inputs(x, w, residual, total, stream):
 
 def allegro_rms_norm_forward(x, w, residual=None, eps: float = 1e-6, total=None, out=None, rstd=None, stream=None):
     """Returns (y [M, C], total [M, C], rstd [M]): total = x + residual (x itself without a residual), y = total *
-    rstd * w with rstd = 1 / sqrt(mean(total^2) + eps).  total and rstd are what the backward takes."""
+    rstd * w with rstd = 1 / sqrt(mean(total^2) + eps).  total and rstd are what the backward takes.  The tensor passed
+    for total may be x or residual itself."""
     code, index, args, total = _norm_inputs(x, w, residual, total, stream)
     shape, dt = x.shape, x.dtype
     m, c = shape

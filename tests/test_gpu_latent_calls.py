@@ -198,3 +198,25 @@ def test_norm_of_many_long_rows(at):
         assert bool((q[s] == want.view(torch.uint8)).all()) and bool((scale.view(m // n, n, 3)[s] == want_scale).all()), s
     del q, scale
     torch.cuda.empty_cache()
+
+
+# ------------------------------------------------------------------- aliases
+
+@pytest.mark.parametrize("dtype", [torch.float32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("m,c", [(500, 3), (500, 65), (300, 1031), (40, 4096), (40, 4097), (5000, 4100), (9, 65536)])
+def test_norm_in_place_of_an_operand(at, dtype, m, c):
+    """total written over x or over the residual: the results of the call with a tensor of its own."""
+    _note(f"[gpu] norm with total in place M={m} C={c} {dtype}")
+    gen = _gen(c)
+    x, r = (_normal(gen, m, c, dtype=dtype).to(DEV) for _ in range(2))
+    w = (1 + _normal(gen, c, scale=0.3)).to(DEV)
+    want = at.allegro_rms_norm_forward(x, w, r)
+    want8 = at.allegro_rms_norm_fp8(x, w, r)
+    for i in (0, 1):
+        args = [x.clone(), r.clone()]
+        y, total, rstd = at.allegro_rms_norm_forward(args[0], w, args[1], total=args[i])
+        assert total is args[i] and all(torch.equal(a, b) for a, b in zip((y, total, rstd), want))
+        args = [x.clone(), r.clone()]
+        q, scale, total = at.allegro_rms_norm_fp8(args[0], w, args[1], total=args[i])
+        assert torch.equal(q.view(torch.uint8), want8[0].view(torch.uint8)) and torch.equal(scale, want8[1])
+        assert torch.equal(total, want8[2])
