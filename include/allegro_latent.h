@@ -68,7 +68,7 @@
  * allegro_latent_last_error().  Host checks: null or misaligned pointers,
  * negative sizes, row strides below the width, M >= 2^31, widths outside
  * 1 .. 65536, G outside 1 .. 1024, unknown dtype or act, workspaces that are too
- * small.  M == 0 succeeds: weight gradients and offsets are zero, nothing else
+ * small, an output of a product at the address of an input.  M == 0 succeeds: weight gradients and offsets are zero, nothing else
  * is written.  Every sum has a fixed order: results are bit-identical run to run
  * on one kind of device.
  */

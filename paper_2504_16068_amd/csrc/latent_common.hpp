@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <initializer_list>
 
 #include "allegro_latent.h"
 #include "plan.hpp"
@@ -73,6 +74,12 @@ inline int check_rows(const void *p, const char *name, int64_t ld, int width, in
     return fail(ALLEGRO_E_INVALID, "%s has row stride %lld, below its width %d", name, (long long)ld, width);
   if (ld > (int64_t(1) << 31)) return fail(ALLEGRO_E_INVALID, "%s has row stride %lld, over 2^31", name, (long long)ld);
   return check_ptr(p, name, elem);
+}
+// An output that is one of the inputs that are read while, or after, it is written.
+inline int check_apart(const void *out, const char *name, std::initializer_list<const void *> inputs) {
+  for (const void *in : inputs)
+    if (out && out == in) return fail(ALLEGRO_E_INVALID, "%s is also an input", name);
+  return ALLEGRO_OK;
 }
 inline int check_width(int v, const char *name) {
   if (v < 1 || v > kMaxWidth) return fail(ALLEGRO_E_INVALID, "%s=%d is not in 1 .. %d", name, v, kMaxWidth);

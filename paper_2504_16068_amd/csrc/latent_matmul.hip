@@ -1775,7 +1775,8 @@ int allegro_grouped_matmul(int dtype, int act, int64_t M, int K, int N, int G, c
   if (M == 0) return ALLEGRO_OK;
   const int e = dtype == ALLEGRO_F32 ? 4 : 2;
   if ((rc = check_ptr(offsets, "offsets", 8)) || (rows && (rc = check_ptr(rows, "rows", 4))) ||
-      (rc = check_rows(X, "X", ldx, K, e)) || (rc = check_ptr(W, "W", e)) || (rc = check_rows(Y, "Y", ldy, N, e)))
+      (rc = check_rows(X, "X", ldx, K, e)) || (rc = check_ptr(W, "W", e)) || (rc = check_rows(Y, "Y", ldy, N, e)) ||
+      (rc = check_apart(Y, "Y", {X, W})))
     return rc;
   const ProductArgs g{M, K, N, G, offsets, rows, X, ldx, W, Y, ldy, nullptr, 0, act, 0, 0, 0};
   hipStream_t s = static_cast<hipStream_t>(stream);
@@ -1825,6 +1826,8 @@ int allegro_grouped_matmul_backward(int dtype, int act, int64_t M, int K, int N,
     z = weight_shape(dtype, M, K, N, G);
     if ((rc = check_workspace(workspace, workspace_bytes, size_t(z.slots) * size_t(z.slot) * sizeof(float)))) return rc;
   }
+  // dX is written before dW reads X
+  if ((rc = check_apart(dX, "dX", {dY, W, dW ? X : nullptr})) || (rc = check_apart(dW, "dW", {X, dY}))) return rc;
   if (dX) {
     // the same product with W transposed: the contraction runs along dY's columns
     const ProductArgs g{M, N, K, G, offsets, rows, dY, lddy, W, dX, lddx, act ? X : nullptr, ldx, 0, 0, 0, 0};
@@ -1853,7 +1856,7 @@ int allegro_grouped_matmul_fp8(int64_t M, int K, int N, int G, const int64_t *of
   if (M == 0) return ALLEGRO_OK;
   if ((offsets && (rc = check_ptr(offsets, "offsets", 8))) || (rows && (rc = check_ptr(rows, "rows", 4))) ||
       (rc = check_rows(X, "X", ldx, K, 1)) || (rc = check_ptr(xs, "xs", 4)) || (rc = check_ptr(W, "W", 1)) ||
-      (rc = check_ptr(ws, "ws", 4)) || (rc = check_rows(Y, "Y", ldy, N, 2)))
+      (rc = check_ptr(ws, "ws", 4)) || (rc = check_rows(Y, "Y", ldy, N, 2)) || (rc = check_apart(Y, "Y", {X, xs, W, ws})))
     return rc;
   if (!offsets) rows = nullptr;  // one group, of all rows in their own order
   ProductF8Args g{M,  K,

@@ -1,0 +1,32 @@
+"""Calls of the latent operators that are refused on the host (no GPU), beyond those of test_latent_abi_cpu.py."""
+
+
+import pytest
+
+latent = pytest.importorskip("paper_2504_16068_amd.latent",
+                             reason="libraries not built (run __graft_entry__.build())")
+from paper_2504_16068_amd.binding import ALLEGRO_E_INVALID  # noqa: E402
+
+X, W, Y, DY, DX, DW, WS, OFF, XS, WSC = (0x10000 * i for i in range(1, 11))
+
+
+def _refused(fn, args, *words):
+    rc = fn(*args)
+    message = latent.allegro_latent_last_error()
+    assert rc == ALLEGRO_E_INVALID, (rc, message)
+    for w in words:
+        assert w in message, message
+
+
+def test_products_refuse_an_output_over_an_input():
+    """A workgroup reads rows of its inputs that another has written by then."""
+    lib = latent.library()
+    for out in (X, W):
+        _refused(lib.allegro_grouped_matmul, [0, 0, 100, 64, 64, 4, OFF, None, X, 64, W, out, 64, None], "Y is also an input")
+    # dtype, act, M, K, N, G, offsets, rows, X, ldx, W, dY, lddy, dX, lddx, dW, workspace, bytes, stream
+    for dx, dw, word in ((DY, None, "dX"), (DY, DW, "dX"), (X, DW, "dX"), (W, None, "dX"), (DX, X, "dW"), (None, DY, "dW")):
+        _refused(lib.allegro_grouped_matmul_backward,
+                 [1, 1, 100, 64, 64, 4, OFF, None, X, 64, W, DY, 64, dx, 64, dw, WS, 1 << 30, None], word + " is also an input")
+    for out in (X, XS, W, WSC):
+        _refused(lib.allegro_grouped_matmul_fp8, [10, 128, 64, 4, OFF, None, X, 128, XS, W, WSC, out, 64, None],
+                 "Y is also an input")
