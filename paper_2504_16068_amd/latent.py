@@ -19,7 +19,7 @@ import os
 
 import torch
 
-from .binding import ALLEGRO_OK, AllegroError, _empty, _launch
+from .binding import ALLEGRO_E_INVALID, ALLEGRO_OK, AllegroError, _empty, _launch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liballegro_latent.so")
@@ -79,6 +79,7 @@ def _check(rc: int):
         raise AllegroError(rc, allegro_latent_last_error())
 
 
+_INT_MAX, _INT64_MAX = 2 ** 31 - 1, 2 ** 63 - 1
 _Tensor = torch.Tensor
 _F32, _BF16, _F8, _I32, _I64 = torch.float32, torch.bfloat16, torch.float8_e4m3fn, torch.int32, torch.int64
 
@@ -103,6 +104,8 @@ def _index(t, name):
     index = t.get_device()
     if index < 0:
         raise ValueError(f"{name} must live on a GPU, not on {t.device}")
+    if t.shape[1] > _INT_MAX:
+        raise AllegroError(ALLEGRO_E_INVALID, f"{name} has {t.shape[1]} columns")
     return index
 
 
@@ -144,6 +147,8 @@ def _weights(w, dims):
         raise TypeError("w must be a torch.Tensor")
     if w.dim() != 3:
         raise ValueError(f"w must be [G, {dims}], got shape {tuple(w.shape)}")
+    if max(w.shape) > _INT_MAX:
+        raise AllegroError(ALLEGRO_E_INVALID, f"w has shape {tuple(w.shape)}")
     return w.shape
 
 
@@ -165,9 +170,14 @@ def _scratch(t, need, index, stream):
     return t, t.data_ptr(), t.numel() * t.element_size()
 
 
-def _bytes(fn, *sizes):
+def _bytes(fn, rows, *sizes):
     out = ctypes.c_size_t()
-    _check(fn(*(int(v) for v in sizes), ctypes.byref(out)))
+    rows, sizes = int(rows), [int(v) for v in sizes]
+    # rows is an int64_t in C, the others an int; what does not fit is refused there all the same
+    if max(sizes) > _INT_MAX or min(sizes) < -_INT_MAX or abs(rows) > _INT64_MAX:
+        rows = max(-_INT64_MAX, min(rows, _INT64_MAX))
+        sizes = [max(-_INT_MAX, min(v, _INT_MAX)) for v in sizes]
+    _check(fn(rows, *sizes, ctypes.byref(out)))
     return out.value
 
 

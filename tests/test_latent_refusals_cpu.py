@@ -1,13 +1,18 @@
 """Calls of the latent operators that are refused on the host (no GPU), beyond those of test_latent_abi_cpu.py."""
 
-
 import pytest
 
+torch = pytest.importorskip("torch")
 latent = pytest.importorskip("paper_2504_16068_amd.latent",
                              reason="libraries not built (run __graft_entry__.build())")
 from paper_2504_16068_amd.binding import ALLEGRO_E_INVALID  # noqa: E402
 
 X, W, Y, DY, DX, DW, WS, OFF, XS, WSC = (0x10000 * i for i in range(1, 11))
+
+
+class _OnGpu(torch.Tensor):
+    def get_device(self):
+        return 0
 
 
 def _refused(fn, args, *words):
@@ -30,3 +35,22 @@ def test_products_refuse_an_output_over_an_input():
     for out in (X, XS, W, WSC):
         _refused(lib.allegro_grouped_matmul_fp8, [10, 128, 64, 4, OFF, None, X, 128, XS, W, WSC, out, 64, None],
                  "Y is also an input")
+
+
+def test_sizes_beyond_a_c_int_are_refused():
+    """ctypes takes a number's low 32 bits: 2^32 + 4 groups or columns must not pass for 4."""
+    big = 2 ** 32 + 4
+    for fn, args, word in ((latent.allegro_group_rows_workspace, (10, big), "G="),
+                           (latent.allegro_group_rows_workspace, (10, 4 - 2 ** 32), "G="),
+                           (latent.allegro_group_rows_workspace, (2 ** 64 + 10, 4), "M="),
+                           (latent.allegro_grouped_matmul_workspace, (10, big, 4, 4), "K="),
+                           (latent.allegro_grouped_matmul_workspace, (10, 4, big, 4), "N="),
+                           (latent.allegro_rms_norm_workspace, (10, big), "C=")):
+        with pytest.raises(latent.AllegroError, match=word) as ex:
+            fn(*args)
+        assert ex.value.code == ALLEGRO_E_INVALID
+    wide = torch.empty(1, 1).expand(1, big)  # as wide a tensor as one likes, of one element
+    with pytest.raises(latent.AllegroError, match="columns"):
+        latent._index(wide.as_subclass(_OnGpu), "x")
+    with pytest.raises(latent.AllegroError, match="w has"):
+        latent._weights(torch.empty(1, 1, 1).expand(4, 8, big), "K, N")
