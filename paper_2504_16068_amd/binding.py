@@ -192,20 +192,20 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _launch(fn, index, stream, *args):
-    """fn(*args, stream handle) for tensors of device `index`, which is the current one meanwhile: the handle
-    of a default stream names that of the current device."""
-    if stream is not None:
-        device = getattr(stream, "device", None)  # anything with a cuda_stream will do
-        if device is not None and device.index != index:
-            raise ValueError(f"stream is one of {device}, the tensors live on cuda:{index}")
-        handle = stream.cuda_stream
-    else:
-        handle = _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
-    if _current_device() == index:
-        return fn(*args, handle)
+def _stream(stream, index):
+    """Handle of the stream of a call whose tensors live on device `index`."""
+    if stream is None:
+        return _raw_stream(index) if _raw_stream is not None else torch.cuda.current_stream(index).cuda_stream
+    device = getattr(stream, "device", None)  # anything with a cuda_stream will do
+    if device is not None and device.index != index:
+        raise ValueError(f"stream is one of {device}, the tensors live on cuda:{index}")
+    return stream.cuda_stream
+
+
+def _there(index, fn, *args):
+    """fn(*args) with the tensors' device current: the handle of a default stream names that of the current device."""
     with torch.cuda.device(index):
-        return fn(*args, handle)
+        return fn(*args)
 
 
 def _sizes(plan: Plan, row_ptr, n_edges):
@@ -219,11 +219,13 @@ def allegro_env_embed(plan: Plan, row_ptr, w, Y, env=None, stream=None):
     n, e = _sizes(plan, row_ptr, w.shape[0])
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_env_embed, plan, row_ptr, w, Y, env, stream)
     if env is None:
         env = _empty((n, plan.U, plan.d2), torch.float32, dev.index, stream)
     _need(env, "env", (n, plan.U, plan.d2), torch.float32, dev)
-    _check(_launch(_lib.allegro_env_embed, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(w), _ptr(Y),
-                   _ptr(env)))
+    _check(_lib.allegro_env_embed(plan.handle, n, e, _ptr(row_ptr), _ptr(w), _ptr(Y), _ptr(env),
+                                  _stream(stream, dev.index)))
     return env
 
 
@@ -233,11 +235,13 @@ def allegro_tp_forward(plan: Plan, row_ptr, x, env, path_w, out=None, stream=Non
     _need(x, "x", (e, plan.U, plan.d1), torch.float32, dev)
     _need(env, "env", (n, plan.U, plan.d2), torch.float32, dev)
     _need(path_w, "path_w", (plan.n_paths, plan.U), torch.float32, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_tp_forward, plan, row_ptr, x, env, path_w, out, stream)
     if out is None:
         out, = _like(stream, x)
     _need(out, "out", (e, plan.U, plan.d1), torch.float32, dev)
-    _check(_launch(_lib.allegro_tp_forward, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env),
-                   _ptr(path_w), _ptr(out)))
+    _check(_lib.allegro_tp_forward(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w), _ptr(out),
+                                   _stream(stream, dev.index)))
     return out
 
 
@@ -251,6 +255,8 @@ def allegro_tp_backward(plan: Plan, row_ptr, x, env, path_w, grad_out, w, Y, out
     _need(grad_out, "grad_out", (e, plan.U, plan.d1), torch.float32, dev)
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_tp_backward, plan, row_ptr, x, env, path_w, grad_out, w, Y, outs, stream)
     if outs is None:
         outs = _like(stream, x, env, w, Y)
     gx, genv, gw, gy = outs
@@ -258,8 +264,9 @@ def allegro_tp_backward(plan: Plan, row_ptr, x, env, path_w, grad_out, w, Y, out
     _need(genv, "grad_env", (n, plan.U, plan.d2), torch.float32, dev)
     _need(gw, "grad_w", (e, plan.U), torch.float32, dev)
     _need(gy, "grad_Y", (e, plan.d2), torch.float32, dev)
-    _check(_launch(_lib.allegro_tp_backward, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env),
-                   _ptr(path_w), _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw), _ptr(gy)))
+    _check(_lib.allegro_tp_backward(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w),
+                                    _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw), _ptr(gy),
+                                    _stream(stream, dev.index)))
     return gx, genv, gw, gy
 
 
@@ -281,6 +288,9 @@ def allegro_tp_backward_train(plan: Plan, row_ptr, x, env, path_w, grad_out, w, 
     _need(grad_out, "grad_out", (e, plan.U, plan.d1), torch.float32, dev)
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_tp_backward_train, plan, row_ptr, x, env, path_w, grad_out, w, Y,
+                      outs, workspace, stream)
     if outs is None:
         outs = _like(stream, x, env, w, Y, path_w)
     gx, genv, gw, gy, gpw = outs
@@ -294,9 +304,10 @@ def allegro_tp_backward_train(plan: Plan, row_ptr, x, env, path_w, grad_out, w, 
         workspace = _empty((max(need, 16),), torch.uint8, dev.index, stream)
     if workspace.device != torch.device(dev) or not workspace.is_contiguous():
         raise ValueError("workspace must be a contiguous tensor on the same device")
-    _check(_launch(_lib.allegro_tp_backward_train, dev.index, stream, plan.handle, n, e, _ptr(row_ptr), _ptr(x),
-                   _ptr(env), _ptr(path_w), _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw),
-                   _ptr(gy), _ptr(gpw), _ptr(workspace), workspace.numel() * workspace.element_size()))
+    _check(_lib.allegro_tp_backward_train(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w),
+                                          _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw), _ptr(gy),
+                                          _ptr(gpw), _ptr(workspace), workspace.numel() * workspace.element_size(),
+                                          _stream(stream, dev.index)))
     return gx, genv, gw, gy, gpw
 
 
@@ -311,6 +322,9 @@ def allegro_tp_backward_train_noalloc(plan: Plan, row_ptr, x, env, path_w, grad_
     _need(grad_out, "grad_out", (e, plan.U, plan.d1), torch.float32, dev)
     _need(w, "w", (e, plan.U), torch.float32, dev)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_tp_backward_train_noalloc, plan, row_ptr, x, env, path_w, grad_out, w, Y,
+                      outs, stream)
     if outs is None:
         outs = _like(stream, x, env, w, Y, path_w)
     gx, genv, gw, gy, gpw = outs
@@ -319,9 +333,9 @@ def allegro_tp_backward_train_noalloc(plan: Plan, row_ptr, x, env, path_w, grad_
     _need(gw, "grad_w", (e, plan.U), torch.float32, dev)
     _need(gy, "grad_Y", (e, plan.d2), torch.float32, dev)
     _need(gpw, "grad_path_w", (plan.n_paths, plan.U), torch.float32, dev)
-    _check(_launch(_lib.allegro_tp_backward_train_noalloc, dev.index, stream, plan.handle, n, e, _ptr(row_ptr),
-                   _ptr(x), _ptr(env), _ptr(path_w), _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw),
-                   _ptr(gy), _ptr(gpw)))
+    _check(_lib.allegro_tp_backward_train_noalloc(plan.handle, n, e, _ptr(row_ptr), _ptr(x), _ptr(env), _ptr(path_w),
+                                                  _ptr(grad_out), _ptr(w), _ptr(Y), _ptr(gx), _ptr(genv), _ptr(gw),
+                                                  _ptr(gy), _ptr(gpw), _stream(stream, dev.index)))
     return gx, genv, gw, gy, gpw
 
 
@@ -330,10 +344,12 @@ def allegro_sh_forward(plan: Plan, vec, Y=None, stream=None):
     dev = vec.device
     e = vec.shape[0]
     _need(vec, "vec", (e, 3), torch.float64, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_sh_forward, plan, vec, Y, stream)
     if Y is None:
         Y = _empty((e, plan.d2), torch.float32, dev.index, stream)
     _need(Y, "Y", (e, plan.d2), torch.float32, dev)
-    _check(_launch(_lib.allegro_sh_forward, dev.index, stream, plan.handle, e, _ptr(vec), _ptr(Y)))
+    _check(_lib.allegro_sh_forward(plan.handle, e, _ptr(vec), _ptr(Y), _stream(stream, dev.index)))
     return Y
 
 
@@ -343,11 +359,13 @@ def allegro_sh_backward(plan: Plan, vec, grad_Y, grad_vec=None, stream=None):
     e = vec.shape[0]
     _need(vec, "vec", (e, 3), torch.float64, dev)
     _need(grad_Y, "grad_Y", (e, plan.d2), torch.float32, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_sh_backward, plan, vec, grad_Y, grad_vec, stream)
     if grad_vec is None:
         grad_vec = _empty((e, 3), torch.float64, dev.index, stream)
     _need(grad_vec, "grad_vec", (e, 3), torch.float64, dev)
-    _check(_launch(_lib.allegro_sh_backward, dev.index, stream, plan.handle, e, _ptr(vec), _ptr(grad_Y),
-                   _ptr(grad_vec)))
+    _check(_lib.allegro_sh_backward(plan.handle, e, _ptr(vec), _ptr(grad_Y), _ptr(grad_vec),
+                                    _stream(stream, dev.index)))
     return grad_vec
 
 
@@ -394,15 +412,18 @@ def allegro_layer_forward(plan: Plan, L: int, H: int, row_ptr, h, V, Y, weights,
                           saved=None, stream=None):
     """Returns (h_out, V_out, saved); weights maps A, W, Mix, B1, B2 to device tensors."""
     dev, n, e = _layer_inputs(plan, L, H, row_ptr, h, V, Y, weights)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_layer_forward, plan, L, H, row_ptr, h, V, Y, weights, h_out,
+                      V_out, saved, stream)
     sv_need, _ = allegro_layer_buffers(plan, L, H, n, e)
     h_out = _like(stream, h)[0] if h_out is None else h_out
     V_out = _like(stream, V)[0] if V_out is None else V_out
     _need(h_out, "h_out", (e, L), torch.float32, dev)
     _need(V_out, "V_out", (e, plan.U, plan.d1), torch.float32, dev)
     saved = _bytes_buffer(saved, sv_need, "saved", dev, stream)
-    _check(_launch(_lib.allegro_layer_forward, dev.index, stream, plan.handle, int(L), int(H), n, e, _ptr(row_ptr),
-                   _ptr(h), _ptr(V), _ptr(Y), *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(h_out), _ptr(V_out),
-                   _ptr(saved), _nbytes(saved)))
+    _check(_lib.allegro_layer_forward(plan.handle, int(L), int(H), n, e, _ptr(row_ptr), _ptr(h), _ptr(V), _ptr(Y),
+                                      *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(h_out), _ptr(V_out),
+                                      _ptr(saved), _nbytes(saved), _stream(stream, dev.index)))
     return h_out, V_out, saved
 
 
@@ -412,6 +433,9 @@ def allegro_layer_backward(plan: Plan, L: int, H: int, row_ptr, h, V, Y, weights
     dev, n, e = _layer_inputs(plan, L, H, row_ptr, h, V, Y, weights)
     _need(dh_out, "dh_out", (e, L), torch.float32, dev)
     _need(dV_out, "dV_out", (e, plan.U, plan.d1), torch.float32, dev)
+    if _current_device() != dev.index:
+        return _there(dev.index, allegro_layer_backward, plan, L, H, row_ptr, h, V, Y, weights, saved,
+                      dh_out, dV_out, outs, workspace, stream)
     _, ws_need = allegro_layer_buffers(plan, L, H, n, e)
     if outs is None:
         inputs = {"h": h, "V": V, "Y": Y, **{k: weights[k] for k in LAYER_WEIGHTS}}
@@ -422,8 +446,9 @@ def allegro_layer_backward(plan: Plan, L: int, H: int, row_ptr, h, V, Y, weights
     for name, shape in layer_weight_shapes(plan, L, H).items():
         _need(outs[name], "d" + name, shape, torch.float32, dev)
     workspace = _bytes_buffer(workspace, ws_need, "workspace", dev, stream)
-    _check(_launch(_lib.allegro_layer_backward, dev.index, stream, plan.handle, int(L), int(H), n, e, _ptr(row_ptr),
-                   _ptr(h), _ptr(V), _ptr(Y), *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(saved), _nbytes(saved),
-                   _ptr(dh_out), _ptr(dV_out), _ptr(outs["h"]), _ptr(outs["V"]), _ptr(outs["Y"]),
-                   *(_ptr(outs[k]) for k in LAYER_WEIGHTS), _ptr(workspace), _nbytes(workspace)))
+    _check(_lib.allegro_layer_backward(plan.handle, int(L), int(H), n, e, _ptr(row_ptr), _ptr(h), _ptr(V), _ptr(Y),
+                                       *(_ptr(weights[k]) for k in LAYER_WEIGHTS), _ptr(saved), _nbytes(saved),
+                                       _ptr(dh_out), _ptr(dV_out), _ptr(outs["h"]), _ptr(outs["V"]), _ptr(outs["Y"]),
+                                       *(_ptr(outs[k]) for k in LAYER_WEIGHTS), _ptr(workspace), _nbytes(workspace),
+                                       _stream(stream, dev.index)))
     return outs

@@ -19,7 +19,7 @@ import os
 
 import torch
 
-from .binding import ALLEGRO_E_INVALID, ALLEGRO_OK, AllegroError, _empty, _launch
+from .binding import ALLEGRO_E_INVALID, ALLEGRO_OK, AllegroError, _current_device, _empty, _stream, _there
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liballegro_latent.so")
@@ -104,8 +104,6 @@ def _index(t, name):
     index = t.get_device()
     if index < 0:
         raise ValueError(f"{name} must live on a GPU, not on {t.device}")
-    if t.shape[1] > _INT_MAX:
-        raise AllegroError(ALLEGRO_E_INVALID, f"{name} has {t.shape[1]} columns")
     return index
 
 
@@ -147,9 +145,10 @@ def _weights(w, dims):
         raise TypeError("w must be a torch.Tensor")
     if w.dim() != 3:
         raise ValueError(f"w must be [G, {dims}], got shape {tuple(w.shape)}")
-    if max(w.shape) > _INT_MAX:
-        raise AllegroError(ALLEGRO_E_INVALID, f"w has shape {tuple(w.shape)}")
-    return w.shape
+    shape = w.shape
+    if shape[0] > _INT_MAX:  # widths are seen by the library as row strides too, which are of 64 bits
+        raise AllegroError(ALLEGRO_E_INVALID, f"w has {shape[0]} groups")
+    return shape
 
 
 def _groups(offsets, rows, g, m, index):
@@ -196,6 +195,8 @@ def allegro_group_rows(types, n_groups: int, offsets=None, rows=None, workspace=
     m, g, index = types.numel(), int(n_groups), types.get_device()
     if index < 0:
         raise ValueError(f"types must live on a GPU, not on {types.device}")
+    if _current_device() != index:
+        return _there(index, allegro_group_rows, types, n_groups, offsets, rows, workspace, stream)
     need = allegro_group_rows_workspace(m, g)
     if offsets is None:
         offsets = _empty((g + 1,), _I64, index, stream)
@@ -204,7 +205,7 @@ def allegro_group_rows(types, n_groups: int, offsets=None, rows=None, workspace=
     t_p = _whole(types, "types", (m,), _I32, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
     keep, ws, ws_bytes = _scratch(workspace, need, index, stream)
-    _check(_launch(_lib.allegro_group_rows, index, stream, m, g, t_p, o_p, r_p, ws, ws_bytes))
+    _check(_lib.allegro_group_rows(m, g, t_p, o_p, r_p, ws, ws_bytes, _stream(stream, index)))
     return offsets, rows
 
 
@@ -214,6 +215,8 @@ def allegro_grouped_matmul(x, w, offsets, rows=None, act: int = ALLEGRO_ACT_NONE
     """Returns y [M, N]: act(x[r]) @ w[type of r] for x [M, K] and w [G, K, N]; zeros for rows without a type."""
     g, _, n = _weights(w, "K, N")
     code, index = _matrix(x, "x")
+    if _current_device() != index:
+        return _there(index, allegro_grouped_matmul, x, w, offsets, rows, act, out, stream)
     dt, shape = x.dtype, x.shape
     m, k = shape
     if out is None:
@@ -221,8 +224,8 @@ def allegro_grouped_matmul(x, w, offsets, rows=None, act: int = ALLEGRO_ACT_NONE
     w_p = _whole(w, "w", (g, k, n), dt, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
     ldx, ldy = _rows(x, "x", shape, dt, index), _rows(out, "out", (m, n), dt, index)
-    _check(_launch(_lib.allegro_grouped_matmul, index, stream, code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx,
-                   w_p, out.data_ptr(), ldy))
+    _check(_lib.allegro_grouped_matmul(code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, w_p, out.data_ptr(), ldy,
+                                       _stream(stream, index)))
     return out
 
 
@@ -236,6 +239,9 @@ def allegro_grouped_matmul_backward(x, w, dy, offsets, rows=None, act: int = ALL
     """Returns (dx [M, K], dw [G, K, N]) of allegro_grouped_matmul; None for one that is not needed."""
     g, _, n = _weights(w, "K, N")
     code, index = _matrix(x, "x")
+    if _current_device() != index:
+        return _there(index, allegro_grouped_matmul_backward, x, w, dy, offsets, rows, act, dx, dw, need_dx,
+                      need_dw, workspace, stream)
     dt, shape = x.dtype, x.shape
     m, k = shape
     w_p = _whole(w, "w", (g, k, n), dt, index)
@@ -251,8 +257,9 @@ def allegro_grouped_matmul_backward(x, w, dy, offsets, rows=None, act: int = ALL
             dw = _empty((g, k, n), dt, index, stream)
         dw_p = _whole(dw, "dw", (g, k, n), dt, index)
         keep, ws, ws_bytes = _scratch(workspace, allegro_grouped_matmul_workspace(m, k, n, g), index, stream)
-    _check(_launch(_lib.allegro_grouped_matmul_backward, index, stream, code, act, m, k, n, g, o_p, r_p, x.data_ptr(),
-                   ldx, w_p, dy.data_ptr(), lddy, dx_p, lddx, dw_p, ws, ws_bytes))
+    _check(_lib.allegro_grouped_matmul_backward(code, act, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, w_p,
+                                                dy.data_ptr(), lddy, dx_p, lddx, dw_p, ws, ws_bytes,
+                                                _stream(stream, index)))
     return dx if need_dx else None, dw if need_dw else None
 
 
@@ -262,6 +269,8 @@ def allegro_grouped_matmul_fp8(x, x_scale, w, w_scale, offsets=None, rows=None, 
     if not isinstance(x, _Tensor):
         raise TypeError("x must be a torch.Tensor")
     index, shape = _index(x, "x"), x.shape
+    if _current_device() != index:
+        return _there(index, allegro_grouped_matmul_fp8, x, x_scale, w, w_scale, offsets, rows, out, stream)
     m, k = shape
     g, n, _ = _weights(w, "N, K")
     kb, nb = (k + SCALE_BLOCK - 1) // SCALE_BLOCK, (n + SCALE_BLOCK - 1) // SCALE_BLOCK
@@ -272,8 +281,8 @@ def allegro_grouped_matmul_fp8(x, x_scale, w, w_scale, offsets=None, rows=None, 
     ws_p = _whole(w_scale, "w_scale", (g, nb, kb), _F32, index)
     o_p, r_p = _groups(offsets, rows, g, m, index)
     ldx, ldy = _rows(x, "x", shape, _F8, index), _rows(out, "out", (m, n), _BF16, index)
-    _check(_launch(_lib.allegro_grouped_matmul_fp8, index, stream, m, k, n, g, o_p, r_p, x.data_ptr(), ldx, xs_p, w_p,
-                   ws_p, out.data_ptr(), ldy))
+    _check(_lib.allegro_grouped_matmul_fp8(m, k, n, g, o_p, r_p, x.data_ptr(), ldx, xs_p, w_p, ws_p, out.data_ptr(),
+                                           ldy, _stream(stream, index)))
     return out
 
 
@@ -299,6 +308,8 @@ def allegro_rms_norm_forward(x, w, residual=None, eps: float = 1e-6, total=None,
     rstd * w with rstd = 1 / sqrt(mean(total^2) + eps).  total and rstd are what the backward takes.  The tensor passed
     for total may be x or residual itself."""
     code, index, args, total = _norm_inputs(x, w, residual, total, stream)
+    if _current_device() != index:
+        return _there(index, allegro_rms_norm_forward, x, w, residual, eps, total, out, rstd, stream)
     shape, dt = x.shape, x.dtype
     m, c = shape
     if out is None:
@@ -306,13 +317,15 @@ def allegro_rms_norm_forward(x, w, residual=None, eps: float = 1e-6, total=None,
     if rstd is None:
         rstd = _empty((m,), _F32, index, stream)
     rstd_p, ldy = _whole(rstd, "rstd", (m,), _F32, index), _rows(out, "out", shape, dt, index)
-    _check(_launch(_lib.allegro_rms_norm_forward, index, stream, code, m, c, eps, *args, out.data_ptr(), ldy, rstd_p))
+    _check(_lib.allegro_rms_norm_forward(code, m, c, eps, *args, out.data_ptr(), ldy, rstd_p, _stream(stream, index)))
     return out, x if total is None else total, rstd
 
 
 def allegro_rms_norm_fp8(x, w, residual=None, eps: float = 1e-6, total=None, q=None, scale=None, stream=None):
     """Returns (q [M, C] float8_e4m3fn, scale [M, ceil(C/128)], total [M, C]): the norm as q * scale."""
     code, index, args, total = _norm_inputs(x, w, residual, total, stream)
+    if _current_device() != index:
+        return _there(index, allegro_rms_norm_fp8, x, w, residual, eps, total, q, scale, stream)
     shape = x.shape
     m, c = shape
     blocks = (c + SCALE_BLOCK - 1) // SCALE_BLOCK
@@ -321,7 +334,7 @@ def allegro_rms_norm_fp8(x, w, residual=None, eps: float = 1e-6, total=None, q=N
     if scale is None:
         scale = _empty((m, blocks), _F32, index, stream)
     scale_p, ldq = _whole(scale, "scale", (m, blocks), _F32, index), _rows(q, "q", shape, _F8, index)
-    _check(_launch(_lib.allegro_rms_norm_fp8, index, stream, code, m, c, eps, *args, q.data_ptr(), ldq, scale_p))
+    _check(_lib.allegro_rms_norm_fp8(code, m, c, eps, *args, q.data_ptr(), ldq, scale_p, _stream(stream, index)))
     return q, scale, x if total is None else total
 
 
@@ -334,6 +347,8 @@ def allegro_rms_norm_backward(total, w, rstd, dy, dtotal=None, dx=None, dw=None,
     """Returns (dx [M, C], dw [C]): dx is the gradient of x and of the residual alike, with dtotal, the gradient
     that reaches total along the residual, added."""
     code, index = _matrix(total, "total")
+    if _current_device() != index:
+        return _there(index, allegro_rms_norm_backward, total, w, rstd, dy, dtotal, dx, dw, workspace, stream)
     dt, shape = total.dtype, total.shape
     m, c = shape
     w_p, rstd_p = _whole(w, "w", (c,), _F32, index), _whole(rstd, "rstd", (m,), _F32, index)
@@ -347,6 +362,6 @@ def allegro_rms_norm_backward(total, w, rstd, dy, dtotal=None, dx=None, dw=None,
         dw = _empty((c,), _F32, index, stream)
     dw_p, lddx = _whole(dw, "dw", (c,), _F32, index), _rows(dx, "dx", shape, dt, index)
     keep, ws, ws_bytes = _scratch(workspace, allegro_rms_norm_workspace(m, c), index, stream)
-    _check(_launch(_lib.allegro_rms_norm_backward, index, stream, code, m, c, total.data_ptr(), ldt, w_p, rstd_p,
-                   dy.data_ptr(), lddy, ds_p, ldds, dx.data_ptr(), lddx, dw_p, ws, ws_bytes))
+    _check(_lib.allegro_rms_norm_backward(code, m, c, total.data_ptr(), ldt, w_p, rstd_p, dy.data_ptr(), lddy, ds_p,
+                                          ldds, dx.data_ptr(), lddx, dw_p, ws, ws_bytes, _stream(stream, index)))
     return dx, dw

@@ -72,8 +72,8 @@ def calls(monkeypatch):
     monkeypatch.setattr(torch.cuda, "stream", stream)
     monkeypatch.setattr(torch.cuda, "device", device)
     monkeypatch.setattr(binding, "_raw_stream", lambda index: CURRENT)
-    monkeypatch.setattr(binding, "_current_device", lambda: rec.device)
     for module in (binding, latent):
+        monkeypatch.setattr(module, "_current_device", lambda: rec.device)
         monkeypatch.setattr(module, "_lib", _Lib(module.library(), rec))
     return rec
 

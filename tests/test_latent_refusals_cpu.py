@@ -10,11 +10,6 @@ from paper_2504_16068_amd.binding import ALLEGRO_E_INVALID  # noqa: E402
 X, W, Y, DY, DX, DW, WS, OFF, XS, WSC = (0x10000 * i for i in range(1, 11))
 
 
-class _OnGpu(torch.Tensor):
-    def get_device(self):
-        return 0
-
-
 def _refused(fn, args, *words):
     rc = fn(*args)
     message = latent.allegro_latent_last_error()
@@ -49,8 +44,8 @@ def test_sizes_beyond_a_c_int_are_refused():
         with pytest.raises(latent.AllegroError, match=word) as ex:
             fn(*args)
         assert ex.value.code == ALLEGRO_E_INVALID
-    wide = torch.empty(1, 1).expand(1, big)  # as wide a tensor as one likes, of one element
-    with pytest.raises(latent.AllegroError, match="columns"):
-        latent._index(wide.as_subclass(_OnGpu), "x")
-    with pytest.raises(latent.AllegroError, match="w has"):
-        latent._weights(torch.empty(1, 1, 1).expand(4, 8, big), "K, N")
+    with pytest.raises(latent.AllegroError, match="groups"):
+        latent._weights(torch.empty(1, 1, 1).expand(big, 1, 1), "K, N")
+    # a tensor's width is its row stride too, which C takes in 64 bits
+    _refused(latent.library().allegro_rms_norm_forward, [0, 1, 4, 1e-6, X, big, None, 0, W, None, 0, Y, big, None, None],
+             "row stride")
