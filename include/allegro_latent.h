@@ -140,6 +140,7 @@ int allegro_rms_norm_backward(int dtype, int64_t M, int C, const void *total, in
 /* Y [M][N] in bf16 from 8-bit X [M][K] with scales xs [M][(K+127)/128] and
  * 8-bit W [G][N][K] with scales ws [G][(N+127)/128][(K+127)/128].  offsets may
  * be NULL with G == 1: every row is then in the one group (rows is ignored).
+ * A product of two scales is formed first, in fp32, and has to be in its range.
  * The 8-bit matrix instructions add each 8 products in units of 2^-13 of the
  * largest (typically 2e-6 of a sum's terms, at most 7 2^-13 of them), the rest is
  * in fp32: hence no fp32 output. */

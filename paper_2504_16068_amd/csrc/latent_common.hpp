@@ -25,7 +25,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // The same, and four floats, at any address that suits 16-bit (or 32-bit)
 // elements: rows of odd widths and strides are read and written 16 bytes at a
 // time too, which the memory path takes without a detour.
-typedef uint32_t u32_any __attribute__((aligned(2)));
 typedef uint32_t u32x2_any __attribute__((ext_vector_type(2), aligned(2)));
 typedef uint32_t u32x4_any __attribute__((ext_vector_type(4), aligned(2)));
 typedef uint32_t u32x4_any8 __attribute__((ext_vector_type(4), aligned(1)));

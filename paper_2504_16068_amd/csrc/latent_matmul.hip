@@ -132,11 +132,12 @@ __device__ __forceinline__ int64_t xcd_order(int64_t b, int64_t n) {
 // --------------------------------------------------- operands in LDS
 // fp32 operands are split into three bf16 parts each, x = h + m + l (8 bits of
 // the significand in each, all exact), and of the nine products of the parts the
-// six of weight 2^-16 and more are summed; the dropped ones are below 2^-26 of
-// the product.  The bf16 matrix instructions take subnormals as zero, hence
-// kScale, and round their sums down, hence every step's sum starts from zero and
-// is added to the running one by the vector units, and every other row (or step)
-// enters negated, so that what is left of the bias cancels over rows.  A sum that
+// six with h, and m m, are summed; the dropped ones are below 2^-24 of the product
+// (|m| is at most 2^-8 of x and |l| 2^-17).  kScale keeps the parts of small values
+// above bf16's subnormals, which hold fewer bits.  The matrix instructions round
+// their sums down, hence every step's sum starts from zero and is added to the
+// running one by the vector units, and every other row (or step) enters negated,
+// so that what is left of the bias cancels over rows.  A sum that
 // is not finite (infinities, NaN, values beyond the scale) is formed again with
 // the fp32 matrix instructions.
 constexpr float kScale = 0x1p24f, kUnscale = 0x1p-48f;
@@ -186,7 +187,11 @@ __device__ __forceinline__ void split_piece(u32x4 v, bool act, float scale, u32x
   o[1] = u32x2{m[0], m[1]};
   o[2] = u32x2{l[0], l[1]};
 }
-__device__ __forceinline__ u32x4 act_piece(u32x4 v, bool act) {  // of bf16 values
+// The same of bf16 values.  SiLU is rounded to bf16 again, the type that the matrix
+// instructions take: with K = 1024 the product is then off by 2.4e-3 of the 64-bit one
+// (2-norm), by 1.7e-3 without, which is the output's rounding; two parts would
+// double the products.
+__device__ __forceinline__ u32x4 act_piece(u32x4 v, bool act) {
   if (act) {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -586,10 +591,12 @@ constexpr bool tile_short(int TN) { return TN != 256; }
 // multiply.
 //
 // Measured (bf16, 100,003 rows of 100 types, K = 1024, N = 512 with SiLU, 105 GFLOP): forward
-// 205 us, 512 TFLOP/s, and the gradient of X 242 us.  Of the latter, contracting 2048
-// instead of 512 columns runs at 855 TFLOP/s: 8 steps are too few to hide a tile's
-// start and its epilogue (512 MB of dY, X and dX, 107 us at the copy rate).  The forward
-// computes each SiLU twice (two tiles of 256 columns).  Few tiles are bound by
+// 205 us, 512 TFLOP/s, and the gradient of X 240 us.  A wave's 64 x 64 of the result reads
+// 16 KB from LDS a step for 32 matrix instructions: of eight waves as many cycles (1,024)
+// as the instructions take, and with one buffer the step's stores come on top.  And of the
+// gradient, contracting 2048 instead of 512 columns runs at 855 TFLOP/s: 8 steps are too
+// few to hide a tile's start and its epilogue (512 MB of dY, X and dX, 107 us at the copy
+// rate).  The forward computes each SiLU twice (two tiles of 256 columns).  Few tiles are bound by
 // the latency of a step: 1.2 us in fp32 (load, split, store to LDS, meet, read,
 // multiply), 1.6 us with one buffer and four waves.
 template <class T, int TN, bool WT, int BUFS>
@@ -1289,7 +1296,6 @@ __device__ __forceinline__ f32x4 block_sum_f8(i32x8 w, i32x8 x) {
 template <int TN>
 __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g) {
   constexpr int KS = 128, MI = 4, NI = TN / 32;
-  
   __shared__ u32x4 x_lds[kTileRows * KS / 16], w_lds[TN * KS / 16];
   __shared__ int srow[kTileRows];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave), l = tid % kWave;
@@ -1415,9 +1421,10 @@ __global__ __launch_bounds__(kThreads, 2) void product_f8_kernel(ProductF8Args g
 // 1152 values for 128 columns.  A wave has 48 rows in flight, its loads a block
 // ahead; a block's sums are scaled as above.
 //
-// Measured: 262,144 rows of 16 types, K = N = 1024 385 us, 1.43 PFLOP/s.  Without its loads and
-// stores it takes 213 us, with the loads alone 302: X is read by 8 workgroups, one for each 128
-// columns, and a block's 24 products of a wave do not cover a load's latency.  Stores
+// Measured: 262,144 rows of 16 types, K = N = 1024 385 us, 1.43 PFLOP/s, bound by its loads: with
+// them alone it takes 302 us, without loads and stores 213.  X is read by 8 workgroups, one for
+// each 128 columns (2.1 GB through L2), and a block's 24 products of a wave do not cover a
+// load's latency.  Stores
 // of 64 bytes a row took 460.
 constexpr int kStreamF8K = kStreamLds / 128;  // longest contraction
 

@@ -32,11 +32,12 @@ constexpr int kThreads = 256, kWaves = kThreads / kWave;
 // earlier steps of the wave, and in lower lanes of its step.  Nothing depends on
 // an order of arrival.
 //
-// Bound by latency: 8 bytes a row (1.05M rows: 8.4 MB, 1.8 us at the copy rate)
-// against three dependent launches, two for few chunks, or one for a single one.  Measured, 1,048,820 rows of
-// 225 types: 3.5 us for the counts, 4.5 for their sums, 10.9 for the places, whose
-// stores are runs of 9 rows; chunks of 4096 or 8192 rows with as many more waves,
-// and neighbouring chunks on one XCD, took as long or longer.
+// 8 bytes a row (1.05M rows: 8.4 MB, 1.8 us at the copy rate) in three dependent
+// launches, two for few chunks, one for a single one.  Measured, 1,048,820 rows of
+// 225 types: 3.5 us for the counts and 4.5 for their sums, both latency, and 10.9 for
+// the places: 8 waves a compute unit, whose lanes store 4 bytes each to runs of 9
+// rows.  Chunks of 4096 or 8192 rows with as many more waves, and neighbouring
+// chunks on one XCD, took as long or longer.
 constexpr int kOneChunk = 4096;  // rows that one workgroup takes alone
 
 __host__ __device__ inline int64_t chunk_rows(int64_t M) {  // at most 1024 chunks
@@ -69,7 +70,7 @@ __device__ __forceinline__ void count_rows(const int32_t *type, int64_t lo, int6
 // Writes rows lo .. hi - 1 (the wave's part) to their places; next[key] is the
 // next free place of each key, advanced in the order of the rows.
 __device__ __forceinline__ void place_rows(const int32_t *type, int64_t lo, int64_t hi, int G, int bits, int *next,
-                                           int32_t *rows, int64_t M, int lane) {
+                                           int32_t *rows, int lane) {
   for (int64_t r0 = lo; r0 < hi; r0 += kWave) {
     const int64_t r = r0 + lane;
     const bool on = r < hi;
@@ -145,7 +146,7 @@ __global__ __launch_bounds__(kThreads) void group_one_kernel(int M, int G, int b
     base += total;
   }
   __syncthreads();
-  place_rows(type, lo, hi, G, bits, count[wave], rows, M, lane);
+  place_rows(type, lo, hi, G, bits, count[wave], rows, lane);
 }
 
 __global__ __launch_bounds__(kThreads) void group_count_kernel(int64_t M, int G, int64_t chunk,
@@ -544,6 +545,8 @@ __device__ __forceinline__ float block_sum(float v, float *tmp, int tid) {
 // One workgroup per row, which it reads twice (the second time from the caches):
 // widths that registers do not hold.  total is written in the second pass, by the
 // thread that reads the element for the last time: it may be x or residual itself.
+// Elements are read one to a lane: 20,000 rows of 8192 fp32 751 us (3.5 TB/s), bf16 560
+// (2.3); backward 1,346 (1.9) and 1,205 (1.1).
 template <class T, bool F8>
 __global__ __launch_bounds__(kThreads) void norm_wide_forward_kernel(NormArgs g) {
   __shared__ float tmp[kWaves];
@@ -780,8 +783,9 @@ __global__ __launch_bounds__(kSumCols *kSumGroups) void column_sum_kernel(int R,
 
 // ------------------------------------------------------------- launches
 constexpr int kMaxBackGroups = 1024;  // partial rows of dw
-// of rows in registers: 8 waves a compute unit (1.05M rows of 128 fp32: 736 us with
-// the forward, 766 with 1024 workgroups; 20,001 of 1031 bf16: 87 and 92)
+// of rows in registers: two to a compute unit, of which registers hold one at a time
+// for the widest rows (1.05M rows of 128 fp32: 736 us with the forward, 766 with 1024
+// workgroups; 20,001 of 1031 bf16: 87 and 92)
 constexpr int kBackGroups = 512;
 
 // Rows in registers up to 64 floats a lane, else one workgroup per row.
@@ -835,8 +839,8 @@ void norm_forward(NormArgs g, hipStream_t s) {
         const int64_t rows = kThreads / z.lanes * norm_rows<vw(), nv(), 16>();
         // rows of one vector a lane: a workgroup for each few rows, in order of arrival
         // (1.05M rows of 128 fp32: 766 us with the backward, 793 with 2048 persistent
-        // workgroups); longer ones: as many workgroups as are resident, as each first
-        // loads its columns' w
+        // workgroups); longer ones: four workgroups to a compute unit (registers hold 1 to
+        // 7 there), as each first loads its columns' w
         const unsigned grid = unsigned(std::min<int64_t>(cdiv(g.M, rows), nv() == 1 ? kMaxGrid : 1024));
         hipLaunchKernelGGL((norm_forward_kernel<T, vw(), nv(), F8>), dim3(grid), dim3(kThreads), 0, s, g);
       }))
