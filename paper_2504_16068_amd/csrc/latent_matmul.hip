@@ -9,7 +9,8 @@
 //   product_f8_kernel         the 8-bit product in tiles
 //   product_f8_stream_kernel  the 8-bit product past weights kept in LDS
 //
-// Measured: one launch alone, under a kernel trace.
+// Measured: one launch alone, under a kernel trace; the smallest and the median of 30
+// where there are two figures.
 //
 // Ragged groups.  The offsets are on the device, so the host launches an upper
 // bound of tiles, M / rows + G + 1, and a workgroup finds its tile by itself: group
@@ -591,7 +592,7 @@ constexpr bool tile_short(int TN) { return TN != 256; }
 // multiply.
 //
 // Measured (bf16, 100,003 rows of 100 types, K = 1024, N = 512 with SiLU, 105 GFLOP): forward
-// 205 us, 512 TFLOP/s, and the gradient of X 240 us.  A wave's 64 x 64 of the result reads
+// 176 to 186 us, 564 TFLOP/s, and the gradient of X 220 to 227 us.  A wave's 64 x 64 of the result reads
 // 16 KB from LDS a step for 32 matrix instructions: of eight waves as many cycles (1,024)
 // as the instructions take, and with one buffer the step's stores come on top.  And of the
 // gradient, contracting 2048 instead of 512 columns runs at 855 TFLOP/s: 8 steps are too
@@ -754,8 +755,8 @@ __global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 && BU
 //
 // Measured: 1,048,820 rows of 16 types, K = 192, N = 128 350 us (1.34 GB, 3.8 TB/s; the six
 // bf16 products of each fp32 one at 0.88 PFLOP/s, close to the rate of a large library
-// product); 523,599 rows, K = 128, N = 64 with SiLU 101 us (4.0 TB/s) and its gradient of X
-// 151 us (0.67 GB, 4.4 TB/s), both bound by memory.  In tiles the first took 411 us.
+// product); 523,599 rows, K = 128, N = 64 with SiLU 97 to 113 us (402 MB, 4.1 TB/s) and its
+// gradient of X 146 to 158 us (0.67 GB, 4.6 TB/s), both bound by memory.  In tiles the first took 411 us.
 constexpr int kStreamThreads = 512, kStreamWaves = kStreamThreads / kWave, kStreamLds = 147456;
 constexpr int kStreamGroups = 256;  // workgroups: one on every compute unit
 
@@ -1042,11 +1043,11 @@ struct WeightArgs {
 // group has more than `range` rows, so the next one's slots start behind it.  BUFS as
 // in product_kernel.
 //
-// Measured: 523,599 rows of 16 types, K = 128, N = 64 fp32 with SiLU 114 us (402 MB, 3.5 TB/s:
-// three workgroups a compute unit have one step of 24 KB each in flight); bf16,
-// 100,003 x 1024 x 512 of 100 types 255 us of 105 GFLOP, where 100 groups of uneven
-// length leave the last of three rounds half empty (one type: 201 us), and both operands'
-// transposing reads fill the LDS.
+// Measured: 523,599 rows of 16 types, K = 128, N = 64 fp32 with SiLU 114 to 130 us (402 MB,
+// 3.5 TB/s: three workgroups a compute unit have one step of 24 KB each in flight); bf16,
+// 100,003 x 1024 x 512 of 100 types 222 to 233 us of 105 GFLOP: both operands' transposing
+// reads fill the LDS, and 100 groups of uneven length leave the last of three rounds half
+// empty (one type: a fifth less).
 template <class T, int TK, int TN, int BUFS>
 __global__ __launch_bounds__(BUFS == 2 ? 512 : tile_threads(TN), TN == 256 ? 4 : 2) void weight_kernel(
     WeightArgs g) {

@@ -409,10 +409,11 @@ struct NormArgs {
 };
 
 // One pass: a row's sum of squares is formed across the lanes that hold it, then the
-// row is scaled, rounded and written from registers (so total may be x or residual).  Bound by memory: 1,048,820 rows of
-// 128 fp32 with residual and total 377 us (2.15 GB, 5.7 TB/s), 523,599 of 256 bf16 to 8
-// bits 178 us (0.95 GB, 5.3 TB/s), 20,001 of 1031 bf16 47 us (165 MB, 3.5 TB/s: rows of odd
-// width end within vectors, and 20,001 rows are five rounds of a workgroup).
+// row is scaled, rounded and written from registers (so total may be x or residual).  Bound by memory (smallest and median of
+// 30, under a kernel trace): 1,048,820 rows of 128 fp32 with residual and total 349 to 359 us
+// (2.15 GB, 6.1 TB/s), 523,599 of 256 bf16 to 8 bits 168 to 179 us (0.95 GB, 5.6 TB/s), 20,001
+// of 1031 bf16 43 us (165 MB, 3.8 TB/s: rows of odd width end within vectors, and 20,001
+// rows are five rounds of a workgroup).
 
 // Rows that a lane has in flight: as many as 16 floats (forward) hold.
 template <int VW, int NV, int FLOATS>
@@ -610,8 +611,8 @@ struct NormBackArgs {
 // dx of a row and its terms of dw in one pass; a lane sums the dw terms of its
 // columns over the rows it visits (a fixed stride), the row groups of a
 // workgroup are then added in order, and the workgroups by column_sum_kernel.
-// Bound by memory: 1,048,820 rows of 128 fp32 371 us (2.15 GB, 5.8 TB/s), 20,001 of 1031 bf16
-// 43 us (165 MB, 3.8 TB/s); the sums 5 us.
+// Bound by memory: 1,048,820 rows of 128 fp32 366 to 375 us (2.15 GB, 5.9 TB/s), 20,001 of
+// 1031 bf16 38 us (165 MB, 4.3 TB/s); the sums 4 to 5 us.
 template <class T, int VW, int NV>
 __global__ __launch_bounds__(kThreads) void norm_backward_kernel(NormBackArgs g) {
   constexpr int kCols = kWave * NV * VW;  // at most: lanes * NV * VW
